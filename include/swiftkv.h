@@ -384,7 +384,7 @@ int32_t swiftkv_debug_bounded_wait(swiftkv_model *m, int64_t limit_clocks, int32
 int32_t swiftkv_debug_fused_barrier_wait(swiftkv_model *m, int64_t limit_clocks, void *cuda_stream);
 
 /* Synchronises `cuda_stream`, then returns and clears the current device's status word of the stand-alone operator
- * entry points below (swiftkv_gemm_tc, swiftkv_attention_prefill): OK, DEVICE_TIMEOUT, ACT_OVERFLOW or CUDA. */
+ * entry points below: OK, DEVICE_TIMEOUT, ACT_OVERFLOW, BAD_TOKEN (an index outside its range) or CUDA. */
 int32_t swiftkv_op_status(void *cuda_stream);
 
 /* Destroys the host object (never the caller's buffers).  Null is allowed. */
@@ -483,6 +483,122 @@ int32_t swiftkv_tail_attention_noalloc(const float *q, const void *k_cache, cons
                                        const int32_t *cu_seqlens, int32_t n_seqs, int32_t max_seq_len,
                                        int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,
                                        void *cuda_stream);
+
+/*
+ * The operators of a verification step over drafted tokens: what a server needs around swiftkv_step's kind of minibatch when
+ * lengths, block tables and drafts live on the device.  In order of use: swiftkv_plan_pages (cache rows of the new tokens),
+ * per layer swiftkv_qk_norm_rope (heads normed and rotated, K / V rows stored) and swiftkv_tree_attention (the new tokens
+ * against the cache and their own ancestors), at the end swiftkv_token_logprobs.  Like the operators above: DEVICE pointers,
+ * queued on `cuda_stream` without synchronising, no allocation; all of them can be captured into a graph.  An index that
+ * the device finds outside its range (a target, a position, a cache row, a page, a length beyond the promised maximum) is
+ * never followed: the call goes on as stated below and swiftkv_op_status reports SWIFTKV_ERR_BAD_TOKEN.
+ */
+
+/* Cache rows of a step's new tokens (pages of SWIFTKV_PAGE_ROWS = 128 rows), planned on the device.
+ *   n_past, n_new, n_owned : int32 [n_seqs]; committed tokens, new tokens, entries in use of the sequence's table row (which
+ *                 may be more than n_past needs: pages kept after rejected drafts); values below 0 read as 0.  n_seqs <= 8192
+ *   block_table : int32 [n_seqs][max_blocks], page numbers
+ *   free_pages  : int32 [free_capacity] with the first *n_free of them free; pages are taken from the end, sequence by sequence
+ * Written:
+ *   block_table_out [n_seqs][max_blocks] : the entries in use, the taken pages behind them, -1 from there on (may be block_table
+ *                 itself; no other output may overlap an input or another output)
+ *   n_owned_out [n_seqs], n_free_out [1], cu_new [n_seqs + 1] : entries in use and free pages afterwards; prefix sums of n_new
+ *   slot_map, positions [max_tokens] : cache row and position of every new token, packed sequence-major; row -1 for a token
+ *                 whose page is missing.  Entries behind the last token are left as they were; tokens beyond max_tokens are not
+ *                 written
+ *   info [4]    : new tokens, pages taken, pages missing, the longest n_past + n_new
+ * With too few free pages earlier sequences are served first.  Deterministic.  Errors: INVALID_ARG, CUDA. */
+int32_t swiftkv_plan_pages(const int32_t *n_past, const int32_t *n_new, const int32_t *n_owned, int32_t n_seqs,
+                           const int32_t *block_table, int32_t max_blocks, const int32_t *free_pages, int32_t free_capacity,
+                           const int32_t *n_free, int32_t *block_table_out, int32_t *n_owned_out, int32_t *n_free_out,
+                           int32_t *cu_new, int32_t *slot_map, int32_t *positions, int32_t max_tokens, int32_t *info,
+                           void *cuda_stream);
+
+/* cos / sin tables fp32 [max_pos][head_dim / 2] of p * theta^(-2i/head_dim), evaluated in double precision (the model's own
+ * table, for swiftkv_qk_norm_rope).  Errors: INVALID_ARG, CUDA. */
+int32_t swiftkv_rope_table(float *cos_tab, float *sin_tab, int32_t max_pos, int32_t head_dim, double theta, void *cuda_stream);
+
+/* Per-head RMSNorm of queries and keys (gain vectors [head_dim] in `dtype`; a null gain: that tensor is not normed), rotary
+ * embedding (rotate-half pairs (i, i + head_dim/2)) and the store of keys and values, in one pass.
+ *   q, k, v   : [n_tokens][heads][head_dim] in `dtype` (F32, BF16, F16); strides in elements between tokens, so that the three
+ *               may be slices of one projection's rows.  head_dim even, <= 256
+ *   positions : int32 [n_tokens] in [0, max_pos) (others are clamped and reported)
+ *   q_out     : [n_tokens][n_q_heads][head_dim] in `dtype`, token stride q_out_stride; may be q with q's stride
+ *   k_cache, v_cache : planes [cache_rows][n_kv_heads][head_dim] in `dtype`; or, with k_scale and v_scale (fp32 [cache_rows]),
+ *               e4m3 codes in the format of SWIFTKV_KV_FP8, quantized from the fp32 row (rows of at most 8192 values)
+ *   slot_map  : int32 [n_tokens], cache row of every token (null: token t goes to row t); a row below 0 is not stored, one at or
+ *               beyond cache_rows neither, and is reported.  No two tokens may name the same row
+ * Everything between load and store is fp32; stores to F16 round like a cast (no clamping).
+ * Errors: INVALID_ARG, UNSUPPORTED (FP8 rows of more than 8192 values), CUDA. */
+int32_t swiftkv_qk_norm_rope(const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                             int32_t dtype, int32_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                             const void *q_gain, const void *k_gain, float eps, const int32_t *positions, const float *cos_tab,
+                             const float *sin_tab, int32_t max_pos, void *q_out, int64_t q_out_stride, void *k_cache, void *v_cache,
+                             float *k_scale, float *v_scale, int32_t cache_rows, const int32_t *slot_map, void *cuda_stream);
+
+/* Its gradient: dq [n_tokens][n_q_heads][head_dim], dk [n_tokens][n_kv_heads][head_dim] (contiguous, `dtype`) are the gradients
+ * of the rotated outputs; q, k, gains, positions and tables as given to the forward call.  dq_in, dk_in (contiguous, `dtype`;
+ * may be dq / dk) receive the gradients of q and k; dq_gain, dk_gain (fp32 [head_dim]; null exactly where the gain is null)
+ * those of the gains, summed over all tokens and heads in a fixed order (no atomics: results repeat bit for bit on one GPU
+ * model).  scratch: >= swiftkv_qk_norm_rope_bwd_scratch_bytes(head_dim) bytes, 16-byte aligned, not shared with a call that may
+ * run at the same time.  (v's gradient is the gradient of the stored values: nothing is computed.)
+ * Errors: INVALID_ARG, WORKSPACE_SMALL, CUDA. */
+size_t  swiftkv_qk_norm_rope_bwd_scratch_bytes(int32_t head_dim);
+int32_t swiftkv_qk_norm_rope_bwd(const void *dq, const void *dk, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                                 int32_t dtype, int32_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                                 const void *q_gain, const void *k_gain, float eps, const int32_t *positions, const float *cos_tab,
+                                 const float *sin_tab, int32_t max_pos, void *dq_in, void *dk_in, float *dq_gain, float *dk_gain,
+                                 void *scratch, size_t scratch_bytes, void *cuda_stream);
+
+/* Attention of several new tokens per sequence -- a tree of drafted tokens, a prompt chunk, or one decode token -- over the
+ * sequence's cache rows, which already hold the new tokens' own K / V.  Sequence b has n_past[b] committed tokens at positions
+ * 0 .. n_past[b] - 1 and its new tokens cu_new[b] .. cu_new[b + 1] - 1 at the positions behind them.  New token i sees every
+ * committed token and the new tokens j whose bit is set in its row of tree_mask (bit j % 32 of word j / 32; its own bit is
+ * not implied), or, with tree_mask null, those with j <= i.  out = softmax(scale q K^T) V, grouped-query; a token that sees
+ * nothing gets zeros and lse = -inf.  What an unseen key's K or V row holds (NaN, infinities) does not matter.
+ *   q           : [total_new][n_q_heads][head_dim] in q_dtype (F32, BF16, F16), q_stride elements between tokens
+ *   k_cache, v_cache : planes [cache_rows][n_kv_heads][head_dim] of q_dtype, or (kv_dtype SWIFTKV_DTYPE_FP8_E4M3) e4m3 codes with
+ *                 k_scale, v_scale fp32 [cache_rows], as swiftkv_kv_cache_view gives them
+ *   block_table : int32 [n_seqs][max_blocks] (position p in row block_table[b][p / 128] * 128 + p % 128), or null and
+ *   row0        : int32 [n_seqs] (position p in row row0[b] + p).  A row outside the cache reads as zeros
+ *   n_past int32 [n_seqs], cu_new int32 [n_seqs + 1], tree_mask int32 [total_new][mask_words]
+ *   max_new, max_kv : at least the largest number of new tokens and of n_past + new tokens of any sequence; a longer sequence is
+ *                 cut there and reported
+ *   out         : [total_new][n_q_heads][head_dim] in q_dtype; lse (nullable): fp32 [total_new][n_q_heads], natural logarithm of the
+ *                 softmax's denominator.  Rows of tokens that belong to no sequence are left as they were
+ *   softmax_scale : 0 means 1/sqrt(head_dim)
+ *   scratch     : >= swiftkv_tree_attention_scratch_bytes(...) bytes (may be null where that is 0), 16-byte aligned, not shared with
+ *                 a call that may run at the same time; sufficient for any smaller total_new and max_kv too
+ * head_dim <= 256.  Errors: INVALID_ARG, WORKSPACE_SMALL, UNSUPPORTED, CUDA. */
+size_t  swiftkv_tree_attention_scratch_bytes(int32_t total_new, int32_t max_kv, int32_t n_q_heads, int32_t head_dim);
+int32_t swiftkv_tree_attention(const void *q, int64_t q_stride, int32_t q_dtype, const void *k_cache, const void *v_cache,
+                               int32_t kv_dtype, const float *k_scale, const float *v_scale, int32_t cache_rows,
+                               const int32_t *block_table, int32_t max_blocks, const int32_t *row0, const int32_t *n_past,
+                               const int32_t *cu_new, const int32_t *tree_mask, int32_t mask_words, void *out, float *lse,
+                               int32_t n_seqs, int32_t total_new, int32_t max_new, int32_t max_kv, int32_t n_q_heads,
+                               int32_t n_kv_heads, int32_t head_dim, float softmax_scale, void *scratch, size_t scratch_bytes,
+                               void *cuda_stream);
+
+/* Per row of logits [rows][vocab] (F32, BF16 or F16; row_stride elements between rows), z = logits / temperature:
+ *   lse = log sum exp z,  logprob = z[target] - lse,  entropy = -sum p log p  (fp32 [rows] each; a logit of -inf adds nothing),
+ *   top_ids int32 / top_logprobs fp32 [rows][top_k], top_k <= 32: the largest logits in descending order, of equal ones the lowest
+ *   index first (0 and -0 are equal; NaN counts as the largest).
+ * targets: int32 [rows] or null; a target below 0 gives logprob 0, one at or beyond vocab the same and is reported.  A row
+ * without any finite logit has lse -inf and NaN elsewhere; one with a NaN or +inf has NaN.
+ * Errors: INVALID_ARG, CUDA. */
+int32_t swiftkv_token_logprobs(const void *logits, int64_t row_stride, int32_t dtype, const int32_t *targets, int32_t rows,
+                               int32_t vocab, float temperature, int32_t top_k, float *logprob, float *entropy, float *lse,
+                               int32_t *top_ids, float *top_logprobs, void *cuda_stream);
+
+/* Its gradient with respect to the logits, from grad_logprob and grad_entropy (fp32 [rows]; grad_entropy nullable):
+ *   d = (grad_logprob (1[target] - p) - grad_entropy p (log p + entropy)) / temperature,  p = exp(z - lse),
+ * with the forward call's lse and entropy; rows whose target is below 0 (or, reported, beyond vocab) get the entropy's part
+ * alone.  grad_logits: `dtype`, grad_stride elements between rows; may be the logits themselves (same pointer and stride).
+ * Errors: INVALID_ARG, CUDA. */
+int32_t swiftkv_token_logprobs_bwd(const void *logits, int64_t row_stride, int32_t dtype, const int32_t *targets, int32_t rows,
+                                   int32_t vocab, float temperature, const float *lse, const float *entropy,
+                                   const float *grad_logprob, const float *grad_entropy, void *grad_logits, int64_t grad_stride,
+                                   void *cuda_stream);
 
 #ifdef __cplusplus
 }

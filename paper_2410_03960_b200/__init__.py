@@ -35,3 +35,13 @@ from .binding import (  # noqa: F401
     workspace_bytes,
 )
 from .flops import prefill_flops  # noqa: F401
+from .verify import (  # noqa: F401
+    op_status,
+    plan_pages,
+    qk_norm_rope,
+    qk_norm_rope_bwd,
+    rope_table,
+    token_logprobs,
+    token_logprobs_bwd,
+    tree_attention,
+)

@@ -28,6 +28,8 @@ EXPORTS = (
     "swiftkv_gemm_tc_split", "swiftkv_attention_prefill_split", "swiftkv_simscore_scratch_bytes", "swiftkv_simscore",
     "swiftkv_distill_workspace_bytes", "swiftkv_distill_grads", "swiftkv_debug_fused_barrier_wait", "swiftkv_adamw_update", "swiftkv_gemm_tf32",
     "swiftkv_half_weight_cache_bytes", "swiftkv_set_half_weight_cache",
+    "swiftkv_plan_pages", "swiftkv_rope_table", "swiftkv_qk_norm_rope", "swiftkv_qk_norm_rope_bwd", "swiftkv_qk_norm_rope_bwd_scratch_bytes",
+    "swiftkv_tree_attention", "swiftkv_tree_attention_scratch_bytes", "swiftkv_token_logprobs", "swiftkv_token_logprobs_bwd",
 )
 
 
@@ -124,6 +126,18 @@ def load_library() -> C.CDLL:
     lib.swiftkv_tail_attention_noalloc.argtypes = [C.c_void_p] * 5 + [C.c_int32] * 6 + [C.c_void_p]
     lib.swiftkv_quantize_rows_fp8.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
     lib.swiftkv_tail_attention_fp8.argtypes = [C.c_void_p] * 7 + [C.c_int32] * 5 + [C.c_void_p, C.c_size_t, C.c_void_p]
+    P, I, L, F = C.c_void_p, C.c_int32, C.c_int64, C.c_float
+    lib.swiftkv_plan_pages.argtypes = [P, P, P, I, P, I, P, I, P, P, P, P, P, P, P, I, P, P]
+    lib.swiftkv_rope_table.argtypes = [P, P, I, I, C.c_double, P]
+    lib.swiftkv_qk_norm_rope.argtypes = [P, L, P, L, P, L, I, I, I, I, I, P, P, F, P, P, P, I, P, L, P, P, P, P, I, P, P]
+    lib.swiftkv_qk_norm_rope_bwd_scratch_bytes.argtypes = [I]
+    lib.swiftkv_qk_norm_rope_bwd_scratch_bytes.restype = C.c_size_t
+    lib.swiftkv_qk_norm_rope_bwd.argtypes = [P, P, P, L, P, L, I, I, I, I, I, P, P, F, P, P, P, I, P, P, P, P, P, C.c_size_t, P]
+    lib.swiftkv_tree_attention_scratch_bytes.argtypes = [I, I, I, I]
+    lib.swiftkv_tree_attention_scratch_bytes.restype = C.c_size_t
+    lib.swiftkv_tree_attention.argtypes = [P, L, I, P, P, I, P, P, I, P, I, P, P, P, P, I, P, P, I, I, I, I, I, I, I, F, P, C.c_size_t, P]
+    lib.swiftkv_token_logprobs.argtypes = [P, L, I, P, I, I, F, I, P, P, P, P, P, P]
+    lib.swiftkv_token_logprobs_bwd.argtypes = [P, L, I, P, I, I, F, P, P, P, P, P, L, P]
     _LIB = lib
     return lib
 

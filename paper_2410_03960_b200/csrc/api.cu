@@ -1245,7 +1245,8 @@ extern "C" int32_t swiftkv_set_split_mask(swiftkv_model *m, int32_t mask) {
 // a device word for the stand-alone entry points' bounded waits
 static __device__ unsigned int g_op_status[64];
 // the word's address on the CURRENT device (every device that loads the library has its own copy of the symbol)
-static unsigned int *op_status_word() {
+namespace skv {
+unsigned int *op_status_word() {
   constexpr int MAX_DEVICES = 64;
   static std::mutex mu;
   static unsigned int *ptr[MAX_DEVICES] = {};
@@ -1258,6 +1259,7 @@ static unsigned int *op_status_word() {
   }
   return ptr[dev];
 }
+}  // namespace skv
 
 extern "C" int32_t swiftkv_op_status(void *cuda_stream) {
   unsigned int *status = op_status_word();
@@ -1269,6 +1271,7 @@ extern "C" int32_t swiftkv_op_status(void *cuda_stream) {
   CUDA_TRY(cudaStreamSynchronize(st));
   if (word & STATUS_TIMEOUT) return fail(SWIFTKV_ERR_DEVICE_TIMEOUT, "a bounded wait inside a stand-alone operator ran out");
   if (word & STATUS_ACT_OVERFLOW) return fail(SWIFTKV_ERR_ACT_OVERFLOW, "a half store of a stand-alone operator was clamped");
+  if (word & STATUS_BAD_TOKEN) return fail(SWIFTKV_ERR_BAD_TOKEN, "a stand-alone operator met an index (target, position, cache row or page) outside its range");
   return SWIFTKV_OK;
 }
 

@@ -107,6 +107,9 @@ __device__ __forceinline__ void store_out(const OutDesc &o, int row, int col, fl
 // the function, so a process that drives several GPUs sets it on each; returns 0 on success
 int ensure_dynamic_smem(const void *kernel, int bytes);
 
+// the current device's status word of the stand-alone operators (null on a CUDA error)
+unsigned int *op_status_word();
+
 // sets the calling thread's swiftkv_last_error() text and returns `code` (defined with the C ABI)
 int32_t report_error(int32_t code, const char *msg);
 

@@ -1,0 +1,831 @@
+"""The verification-step operators on the GPU against 64-bit restatements (verify_reference.py), at the sizes and masks where
+they can go wrong.
+
+Tolerances.  u is half a step of the output's type relative to the value (torch.finfo(t).eps / 2).  An fp32 chain of n
+products and sums adds at most about n 2^-24 of the sum of the magnitudes involved; the approximate exp2 / log2 / rsqrt units
+are good to 2^-22 relative.  Each test states what it multiplies."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import verify_reference as R
+
+pytestmark = pytest.mark.gpu
+
+BF, HF, FF = torch.bfloat16, torch.float16, torch.float32
+THETA, EPS = 500000.0, 1e-5
+
+
+def u_of(dt):
+    return torch.finfo(dt).eps / 2
+
+
+def tiny_of(dt):
+    """Half a step of the type's smallest values: IEEE halves step by 2^-24 below 2^-14, the others by less than 2^-126."""
+    return 2.0 ** -25 if dt == torch.float16 else 1e-37
+
+
+def f64(t):
+    return t.detach().double().cpu().numpy()
+
+
+def i32(values):
+    return torch.tensor(np.asarray(values), dtype=torch.int32, device="cuda")
+
+
+def e4m3(codes):
+    return f64(codes.view(torch.float8_e4m3fn).float())
+
+
+# ------------------------------------------------------------------------------------------------------- plan_pages
+def plan_case(rng, seqs, past_hi, new_hi, extra_blocks=3, scarce=False):
+    past, new = rng.integers(0, past_hi + 1, seqs), rng.integers(0, new_hi + 1, seqs)
+    owned = -(-past // 128) + (rng.random(seqs) < 0.3)
+    blocks = int(max((past + new + 127) // 128 + 1)) + extra_blocks
+    pages = rng.permutation(int(owned.sum()) + 4000)
+    table, at = np.full((seqs, blocks), -7), 0
+    for b in range(seqs):
+        table[b, : owned[b]] = pages[at: at + owned[b]]
+        at += owned[b]
+    need = int(np.maximum(0, -(-(past + new) // 128) - owned).sum())
+    n_free = need // 2 if scarce else need + 5
+    return past, new, owned, table, pages[at: at + max(n_free + 3, 4)], n_free, blocks
+
+
+@pytest.mark.parametrize("seqs,past_hi,new_hi,scarce", [(1, 0, 1, False), (1, 0, 0, False), (1, 500, 700, False), (3, 128, 128, True), (33, 1000, 5, False), (257, 3000, 300, True),
+                                                        (1000, 9000, 40, False), (8192, 200, 2, False), (5, 60000, 9000, False)])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_plan_pages(seqs, past_hi, new_hi, scarce, in_place):
+    import paper_2410_03960_b200 as P
+    past, new, owned, table, free, n_free, blocks = plan_case(np.random.default_rng(seqs + new_hi), seqs, past_hi, new_hi, scarce=scarce)
+    want = R.plan(past, new, owned, table, free, n_free, blocks)
+    room = int(new.sum()) + 9
+    t = i32(table)
+    out = {"block_table": t if in_place else torch.full_like(t, 99), "n_owned": i32([-5] * seqs), "n_free": i32([-5]), "cu_new": i32([-5] * (seqs + 1)),
+           "slot_map": i32([-55] * room), "positions": i32([-55] * room), "info": i32([0] * 4)}
+    got = P.plan_pages(i32(past), i32(new), i32(owned), t, i32(free), i32([n_free]), out=out)
+    P.op_status()
+    n = int(new.sum())
+    for name in ("n_owned", "n_free", "cu_new", "info", "block_table"):
+        assert np.array_equal(got[name].cpu().numpy(), want[name]), name
+    for name in ("slot_map", "positions"):
+        assert np.array_equal(got[name][:n].cpu().numpy(), want[name]), name
+        assert (got[name][n:] == -55).all(), "entries behind the last token"
+
+
+def test_plan_pages_bounds_what_it_finds():
+    """Negative counts read as zero, a table row that is too short and a room that is too small cut what does not fit."""
+    import paper_2410_03960_b200 as P
+    got = P.plan_pages(i32([-3, 250, 100]), i32([-1, 300, 20]), i32([-2, 99, 1]), i32(np.arange(9).reshape(3, 3)), i32([50, 51, 52]), i32([7]), max_tokens=310)
+    assert got["cu_new"].tolist() == [0, 0, 300, 320] and got["n_owned"].tolist() == [0, 3, 1] and got["n_free"].tolist() == [3]
+    assert got["info"].tolist() == [320, 0, 2, 550]
+    slots = got["slot_map"].tolist()
+    assert slots[:6] == [4 * 128 + 122 + i for i in range(6)] and slots[134 - 1] == 5 * 128 + 127 and slots[134:300] == [-1] * 166
+    assert slots[300:310] == [6 * 128 + 100 + i for i in range(10)]
+
+
+# ------------------------------------------------------------------------------------------- qk_norm_rope and gradient
+def rope_inputs(T, n_q, n_kv, hd, dt, seed, strided=True, max_pos=131072):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    width = (n_q + 2 * n_kv) * hd + (8 if strided else 0)
+    x = (torch.randn((T, width), generator=g, device="cuda") * 1.5).to(dt)
+    q, k, v = (x[:, a: a + n * hd].view(T, n, hd) for a, n in ((0, n_q), (n_q * hd, n_kv), ((n_q + n_kv) * hd, n_kv)))
+    pos = torch.randint(0, max_pos, (T,), generator=g, device="cuda", dtype=torch.int32)
+    gains = tuple((1 + 0.3 * torch.randn(hd, generator=g, device="cuda")).to(dt) for _ in range(2))
+    return g, q, k, v, pos, gains
+
+
+def rope_bound(x, gain, pos, u, hd, y, tiny=1e-37):
+    """u |y| for the store; the pair's magnitudes times 2^-24 (sum of hd squares, rsqrt, gain, table entries, two products):
+    hd / 32 + 16 roundings cover the pairwise sums and the chain."""
+    h = np.abs(R.head_norm(x, gain, EPS))
+    lo, hi = h[..., : hd // 2], h[..., hd // 2:]
+    return u * np.abs(y) + (hd / 32 + 16) * 2.0 ** -24 * np.concatenate([lo + hi, lo + hi], -1) + tiny
+
+
+SHAPES = [(1, 1, 1, 2), (3, 4, 2, 32), (7, 6, 2, 64), (5, 5, 1, 80), (33, 32, 8, 128), (4, 10, 2, 256), (2, 3, 3, 250), (129, 8, 8, 128)]
+
+
+@pytest.mark.parametrize("T,n_q,n_kv,hd", SHAPES)
+@pytest.mark.parametrize("dt", [BF, HF, FF])
+@pytest.mark.parametrize("norm", ["both", "k", "none"])
+def test_qk_norm_rope(T, n_q, n_kv, hd, dt, norm):
+    import paper_2410_03960_b200 as P
+    g, q, k, v, pos, (qg, kg) = rope_inputs(T, n_q, n_kv, hd, dt, T * hd, strided=T % 2 == 1)
+    qg, kg = (qg if norm == "both" else None), (kg if norm != "none" else None)
+    cos, sin = P.rope_table(131072, hd, THETA)
+    rows = 2 * T + 3
+    slots = torch.randperm(rows, generator=g, device="cuda")[:T].to(torch.int32)
+    slots[0] = -1                                             # a token whose page is missing
+    kc, vc = torch.full((rows, n_kv, hd), 7.0, dtype=dt, device="cuda"), torch.full((rows, n_kv, hd), 9.0, dtype=dt, device="cuda")
+    out = P.qk_norm_rope(q, k, v, pos, cos, sin, q_gain=qg, k_gain=kg, eps=EPS, k_cache=kc, v_cache=vc, slot_map=slots)
+    P.op_status()
+    p, s, u = pos.cpu().numpy(), slots.cpu().numpy(), u_of(dt)
+    for x, gain, got, stored in ((q, qg, f64(out), np.ones(T, bool)), (k, kg, f64(kc)[np.maximum(s, 0)], s >= 0)):
+        x, gain = f64(x), None if gain is None else f64(gain)
+        want = R.rotate(R.head_norm(x, gain, EPS), p, THETA)
+        bad = (np.abs(got - want) > rope_bound(x, gain, p, u, hd, want, tiny_of(dt))) & stored[:, None, None]
+        assert not bad.any(), np.argwhere(bad)[:4]
+    assert torch.equal(vc[slots[1:].long()], v[1:])
+    left = np.setdiff1d(np.arange(rows), s[s >= 0])
+    assert (kc[left] == 7).all() and (vc[left] == 9).all(), "rows that no token names"
+
+
+@pytest.mark.parametrize("T,n_q,n_kv,hd", [(1, 1, 1, 16), (5, 6, 2, 64), (17, 32, 8, 128), (3, 4, 4, 256), (3, 5, 1, 80), (2, 2, 64, 128)])
+@pytest.mark.parametrize("dt", [BF, HF, FF])
+def test_qk_norm_rope_into_an_fp8_cache(T, n_q, n_kv, hd, dt):
+    """Scales to fp32 accuracy, codes to half a step of e4m3 (2^-4 of the value, 2^-10 of the scale where it is subnormal); the
+    kernel decides from its own fp32 value, whose error is the bound of the plain store."""
+    import paper_2410_03960_b200 as P
+    g, q, k, v, pos, (qg, kg) = rope_inputs(T, n_q, n_kv, hd, dt, 3 * T + hd)
+    if T > 2:
+        v[1] = 0.0                                            # an all-zero row
+    cos, sin = P.rope_table(131072, hd, THETA)
+    rows = T + 4
+    slots = torch.randperm(rows, generator=g, device="cuda")[:T].to(torch.int32)
+    kc, vc = (torch.full((rows, n_kv, hd), 0x11, dtype=torch.uint8, device="cuda") for _ in range(2))
+    ks, vs = (torch.full((rows,), 5.0, device="cuda") for _ in range(2))
+    P.qk_norm_rope(q, k, v, pos, cos, sin, q_gain=qg, k_gain=kg, eps=EPS, k_cache=kc, v_cache=vc, k_scale=ks, v_scale=vs, slot_map=slots)
+    P.op_status()
+    p, s = pos.cpu().numpy(), slots.cpu().numpy()
+    for x, gain, codes, scales in ((f64(k), f64(kg), kc, ks), (f64(v), None, vc, vs)):
+        want = R.rotate(R.head_norm(x, gain, EPS), p, THETA) if gain is not None else x
+        err = rope_bound(x, gain, p, 0.0, hd, want) if gain is not None else np.zeros_like(x)
+        sc = f64(scales)[s]
+        # scale = RN(max(amax, 2^-64) / 448): half a step (2^-24) of that maximum, the floor included -- an all-zero row's scale is
+        # 2^-64 / 448 and rounds too, so the relative term multiplies the floored maximum
+        amax = np.maximum(np.abs(want).reshape(T, -1).max(1), 2.0 ** -64)
+        assert (np.abs(sc * 448 - amax) <= err.reshape(T, -1).max(1) + 2.0 ** -23 * amax).all()
+        got = e4m3(codes)[s] * sc[:, None, None]
+        assert (np.abs(got - want) <= 2.0 ** -4 * np.abs(want) + (2.0 ** -10 + 2.0 ** -20) * sc[:, None, None] + 2 * err).all()
+        left = np.setdiff1d(np.arange(rows), s)
+        assert (codes[left] == 0x11).all() and (scales[left] == 5).all()
+
+
+def test_qk_norm_rope_in_place_and_unaligned():
+    """q_out = q, keys and values "stored" to plain tensors, and tensors that start off a 16-byte boundary: the same bits."""
+    import paper_2410_03960_b200 as P
+    T, n_q, n_kv, hd = 37, 8, 2, 128
+    _, q, k, v, pos, (qg, kg) = rope_inputs(T, n_q, n_kv, hd, BF, 5)
+    cos, sin = P.rope_table(131072, hd, THETA)
+    k1, v1 = (torch.empty((T, n_kv, hd), dtype=BF, device="cuda") for _ in range(2))
+    ref = P.qk_norm_rope(q, k, v, pos, cos, sin, q_gain=qg, k_gain=kg, k_cache=k1, v_cache=v1)
+    flat = torch.empty(T * n_q * hd + 1, dtype=BF, device="cuda")
+    off = flat[1:].view(T, n_q, hd)
+    off.copy_(q)
+    k2, v2 = torch.empty_like(k1), torch.empty_like(v1)
+    got = P.qk_norm_rope(off, k, v, pos, cos, sin, q_gain=qg, k_gain=kg, k_cache=k2, v_cache=v2, q_out=off)
+    assert got.data_ptr() == off.data_ptr()
+    # (two kernels: the same arithmetic up to the order of the sum of squares)
+    assert (got.float() - ref.float()).abs().max() <= 2.0 ** -7 * ref.float().abs().max()
+    qi = q.clone()
+    got = P.qk_norm_rope(qi, k, v, pos, cos, sin, q_gain=qg, k_gain=kg, k_cache=k2, v_cache=v2, q_out=qi)
+    assert torch.equal(got, ref) and torch.equal(k1, k2) and torch.equal(v1, v2)
+    P.op_status()
+
+
+def test_qk_norm_rope_reports_bad_indices():
+    import paper_2410_03960_b200 as P
+    _, q, k, v, pos, _ = rope_inputs(4, 4, 2, 64, BF, 6, max_pos=50)
+    cos, sin = P.rope_table(50, 64, THETA)
+    for bad_pos, bad_slot in ((50, 0), (-1, 0), (0, 10)):
+        pos2, slots = pos.clone(), i32([3, 1, 2, 9])
+        pos2[1] = bad_pos
+        slots[2] = bad_slot if bad_slot else 2
+        kc = torch.zeros((10, 2, 64), dtype=BF, device="cuda")
+        P.qk_norm_rope(q, k, v, pos2, cos, sin, k_cache=kc, v_cache=torch.zeros_like(kc), slot_map=slots)
+        with pytest.raises(P.SwiftKVError) as e:
+            P.op_status()
+        assert e.value.code == -6
+        P.op_status()                                        # reported once
+        assert (kc[0] == 0).all() and (kc[4:9] == 0).all() and (kc[9] != 0).any()
+
+
+@pytest.mark.parametrize("T,n_q,n_kv,hd", [(1, 1, 1, 2), (3, 4, 2, 32), (9, 6, 2, 64), (33, 32, 8, 128), (4, 10, 2, 256), (2, 3, 3, 250), (700, 8, 1, 128)])
+@pytest.mark.parametrize("dt", [BF, HF, FF])
+@pytest.mark.parametrize("norm", ["both", "q", "none"])
+def test_qk_norm_rope_gradient(T, n_q, n_kv, hd, dt, norm):
+    import paper_2410_03960_b200 as P
+    g, q, k, v, pos, (qg, kg) = rope_inputs(T, n_q, n_kv, hd, dt, T + hd, strided=T % 2 == 1)
+    qg, kg = (qg if norm != "none" else None), (kg if norm == "both" else None)
+    dq, dk = ((torch.randn((T, n, hd), generator=g, device="cuda")).to(dt) for n in (n_q, n_kv))
+    cos, sin = P.rope_table(131072, hd, THETA)
+    got = P.qk_norm_rope_bwd(dq, dk, q, k, pos, cos, sin, q_gain=qg, k_gain=kg, eps=EPS)
+    again = P.qk_norm_rope_bwd(dq.clone(), dk.clone(), q, k, pos, cos, sin, q_gain=qg, k_gain=kg, eps=EPS)
+    P.op_status()
+    p, u = pos.cpu().numpy(), u_of(dt)
+    for x, dy, gain, dx, dg in ((q, dq, qg, got[0], got[2]), (k, dk, kg, got[1], got[3])):
+        xn, dn, gn = f64(x), f64(dy), None if gain is None else f64(gain)
+        want, wg = R.norm_rope_bwd(xn, dn, gn, EPS, p, THETA)
+        # the pair's gradient magnitudes, and -- normed -- |x| r times the mean of |dz g xh|, each with the chain's roundings
+        a = np.abs(dn)
+        pair = np.concatenate([a[..., : hd // 2] + a[..., hd // 2:]] * 2, -1)
+        mag = pair
+        if gn is not None:
+            r = 1 / np.sqrt((xn * xn).mean(-1, keepdims=True) + EPS)
+            mag = r * (pair * np.abs(gn) + np.abs(xn) * r * (pair * np.abs(gn) * np.abs(xn) * r).mean(-1, keepdims=True))
+        assert (np.abs(f64(dx) - want) <= u * np.abs(want) + (hd / 32 + 24) * 2.0 ** -24 * mag + tiny_of(dt)).all()
+        if gn is None:
+            assert dg is None
+        else:
+            # fp32 partial sums: a thread's chain of at most tokens * heads / 32 terms, then a tree
+            terms = (pair * np.abs(xn) * r).sum((0, 1))
+            assert (np.abs(f64(dg) - wg) <= (24 + T * x.shape[1] / 32) * 2.0 ** -24 * terms + 1e-30).all()
+    for a, b in zip(got, again):
+        assert (a is None and b is None) or torch.equal(a, b), "repeats bit for bit"
+    P.qk_norm_rope_bwd(dq, dk, q, k, pos, cos, sin, q_gain=qg, k_gain=kg, eps=EPS, out=(dq, dk))       # in place
+    assert torch.equal(dq, got[0]) and torch.equal(dk, got[1])
+
+
+def test_qk_norm_rope_gradient_against_differences():
+    """Directional derivatives of the 64-bit forward formula: |difference quotient - gradient . direction| is at most the
+    quotient's own error (h^2 f''' / 6, about 1e-7 of the terms at h = 1e-4) plus the kernel's 2^-17 of them."""
+    import paper_2410_03960_b200 as P
+    T, n_q, n_kv, hd = 6, 4, 2, 64
+    g, q, k, v, pos, (qg, kg) = rope_inputs(T, n_q, n_kv, hd, FF, 11, strided=False)
+    dq, dk = (torch.randn((T, n, hd), generator=g, device="cuda") for n in (n_q, n_kv))
+    cos, sin = P.rope_table(131072, hd, THETA)
+    gq, gk, gqg, gkg = P.qk_norm_rope_bwd(dq, dk, q, k, pos, cos, sin, q_gain=qg, k_gain=kg, eps=EPS)
+    p = pos.cpu().numpy()
+    rng = np.random.default_rng(0)
+    for x, dy, gain, gx, gg in ((q, dq, qg, gq, gqg), (k, dk, kg, gk, gkg)):
+        x, dy, gain = f64(x), f64(dy), f64(gain)
+        f = lambda x_, g_: float((R.rotate(R.head_norm(x_, g_, EPS), p, THETA) * dy).sum())  # noqa: E731
+        for _ in range(4):
+            d, e = rng.standard_normal(x.shape), rng.standard_normal(gain.shape)
+            num = (f(x + 1e-4 * d, gain + 1e-4 * e) - f(x - 1e-4 * d, gain - 1e-4 * e)) / 2e-4
+            terms = np.abs(f64(gx) * d).sum() + np.abs(f64(gg) * e).sum()
+            assert abs(num - (f64(gx) * d).sum() - (f64(gg) * e).sum()) <= (2.0 ** -17 + 1e-6) * terms
+
+
+# --------------------------------------------------------------------------------------------------- tree_attention
+def random_tree(rng, n, words):
+    """Ancestor sets as bit rows [n, words] and as a matrix."""
+    seen = []
+    for i in range(n):
+        parent = int(rng.integers(-1, i)) if i else -1
+        seen.append((seen[parent] if parent >= 0 else 0) | 1 << i)
+    bits = np.array([[(m >> (32 * w)) & 0xFFFFFFFF for w in range(words)] for m in seen], dtype=np.uint32).reshape(n, words)
+    return bits.view(np.int32), np.array([[bool(m >> j & 1) for j in range(n)] for m in seen]).reshape(n, n)
+
+
+def tree_case(seed, lens, n_q, n_kv, hd, dt, fp8=False, paged=True, mask=True, strided=False):
+    rng = np.random.default_rng(seed)
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    past, new = [a for a, _ in lens], [b for _, b in lens]
+    T, words = sum(new), max(1, -(-max(new) // 32))
+    cu = np.concatenate([[0], np.cumsum(new)]).astype(int)
+    pages = [-(-(p + n) // 128) for p, n in lens]
+    n_pages = sum(pages) + 2
+    cache_rows = n_pages * 128
+    order, at, table, rows, row0 = rng.permutation(n_pages), 0, np.full((len(lens), max(max(pages), 1) + 1), -1), [], []
+    for b, (p, n) in enumerate(lens):
+        if paged:
+            table[b, : pages[b]] = order[at: at + pages[b]]
+            rows.append((table[b, np.arange(p + n) // 128] * 128 + np.arange(p + n) % 128) if p + n else np.zeros(0, int))
+        else:
+            row0.append(at * 128 + int(rng.integers(0, 3)) * 37)
+            rows.append(row0[-1] + np.arange(p + n))
+        at += pages[b]
+    c = dict(T=T, past=past, cu=cu, rows=rows, max_new=max(new), max_kv=max(p + n for p, n in lens), n_q=n_q, n_kv=n_kv, hd=hd, dt=dt, fp8=fp8)
+    q = torch.randn((T, n_q * hd + (8 if strided else 0)), generator=g, device="cuda").mul(1.5).to(dt)
+    c["q"] = q[:, : n_q * hd].view(T, n_q, hd)
+    if fp8:
+        c["k"], c["v"] = (torch.randn((cache_rows, n_kv, hd), generator=g, device="cuda").mul(120).clamp(-448, 448).to(torch.float8_e4m3fn).view(torch.uint8) for _ in range(2))
+        c["ks"], c["vs"] = ((torch.rand(cache_rows, generator=g, device="cuda") + 0.5) / 120 for _ in range(2))
+    else:
+        c["k"], c["v"] = (torch.randn((cache_rows, n_kv, hd), generator=g, device="cuda").to(dt) for _ in range(2))
+        c["ks"] = c["vs"] = None
+    bits, sees = [], []
+    for n in new:
+        m, s = random_tree(rng, n, words)
+        bits.append(m)
+        sees.append(s if mask else np.tril(np.ones((n, n), bool)))
+    c["mask"] = i32(np.concatenate(bits)) if mask else None
+    c["sees"] = sees
+    c["table"], c["row0"] = (i32(table), None) if paged else (None, i32(row0))
+    return c
+
+
+def run_tree(c, **kw):
+    import paper_2410_03960_b200 as P
+    lse = torch.full((c["T"], c["n_q"]), 77.0, device="cuda")
+    args = dict(block_table=c["table"], row0=c["row0"], tree_mask=c["mask"], k_scale=c["ks"], v_scale=c["vs"], lse=lse)
+    args.update(kw)
+    out = P.tree_attention(c["q"], c["k"], c["v"], i32(c["past"]), i32(c["cu"]), c["max_new"], c["max_kv"], **args)
+    return out, lse
+
+
+def check_tree(c, out, lse, scale=None):
+    """|out - o| <= u |o| + (u_P + e) A with A = sum p |v|: u_P the rounding of the probabilities to 16 bits (the 16-bit paths; with an
+    FP8 cache they carry the rows' scale and are bf16), e the relative error of a probability: twice that of its exponent, which is the
+    products' (hd + 2) 2^-24 of sum |q k| scale, plus 2^-20 for exp2 and the fp32 sums over the keys (pairwise inside a tile, then a
+    chain over tiles and splits)."""
+    u = u_of(c["dt"])
+    if c["fp8"]:
+        k, v = e4m3(c["k"]) * f64(c["ks"])[:, None, None], e4m3(c["v"]) * f64(c["vs"])[:, None, None]
+        u_p = 2.0 ** -8 if c["dt"] != FF else 0.0
+    else:
+        k, v = f64(c["k"]), f64(c["v"])
+        u_p = u if c["dt"] != FF else 0.0
+    want, wl, A, Z = R.tree_attention(f64(c["q"]), k, v, c["past"], c["cu"], c["rows"], c["sees"], scale)
+    dz = (c["hd"] + 2) * 2.0 ** -24 * Z + 2.0 ** -20 + 2.0 ** -24 * np.where(np.isfinite(wl), np.abs(wl), 0) * 4
+    keys = c["max_kv"] / 128 + 64
+    e = (2 * dz + keys * 2.0 ** -24)[..., None]
+    got, gl = f64(out), f64(lse)
+    sees = np.isfinite(wl)
+    assert np.array_equal(sees, np.isfinite(gl)) and (gl[~sees] == -np.inf).all() and (got[~sees] == 0).all()
+    bad = np.abs(got - want) > u * np.abs(want) + (u_p * 1.01 + e) * A + tiny_of(c["dt"])
+    assert not bad.any(), (np.argwhere(bad)[:4], np.abs(got - want).max())
+    assert (np.abs(gl - wl)[sees] <= (dz + keys * 2.0 ** -24 + 2.0 ** -22 * (1 + np.abs(np.where(sees, wl, 0))))[sees]).all()
+
+
+LENS = [[(0, 1)], [(127, 1)], [(128, 1)], [(0, 33)], [(700, 1), (0, 5), (130, 7)], [(5, 3), (200, 0), (0, 1), (126, 4)], [(1000, 40), (64, 64)], [(2500, 17)]]
+
+
+@pytest.mark.parametrize("lens", LENS, ids=str)
+@pytest.mark.parametrize("heads", [(8, 2, 128), (4, 4, 64), (32, 8, 128)], ids=str)
+@pytest.mark.parametrize("kind", ["bf16", "f16", "fp8"])
+@pytest.mark.parametrize("paged", [True, False])
+def test_tree_attention(lens, heads, kind, paged):
+    import paper_2410_03960_b200 as P
+    c = tree_case(len(lens) * 100 + lens[0][0], lens, *heads, HF if kind == "f16" else BF, fp8=kind == "fp8", paged=paged, strided=paged)
+    check_tree(c, *run_tree(c))
+    P.op_status()
+
+
+@pytest.mark.parametrize("heads", [(7, 1, 128), (10, 2, 128), (3, 1, 64), (24, 2, 128), (16, 1, 128), (65, 1, 128), (200, 1, 64), (5, 5, 128)], ids=str)
+@pytest.mark.parametrize("kind", ["bf16", "fp8"])
+def test_tree_attention_group_sizes(heads, kind):
+    """Groups that do not divide a tile of 128 query rows, and groups larger than one."""
+    c = tree_case(heads[0], [(300, 23), (129, 1), (90, 50)], *heads, BF, fp8=kind == "fp8")
+    check_tree(c, *run_tree(c))
+
+
+@pytest.mark.parametrize("heads", [(8, 2, 128), (4, 2, 32), (3, 3, 80), (2, 1, 256), (6, 2, 2), (5, 1, 17)], ids=str)
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f32 fp8"])
+def test_tree_attention_other_shapes(heads, kind):
+    c = tree_case(heads[2], [(300, 9), (0, 3), (1500, 2)], *heads, BF if kind == "bf16" else FF, fp8="fp8" in kind, mask=heads[0] != 3)
+    check_tree(c, *run_tree(c))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16", "fp8", "f32"])
+def test_tree_attention_causal_and_scale(kind):
+    c = tree_case(3, [(1029, 130), (0, 257), (3, 1)], 8, 2, 128, {"bf16": BF, "f16": HF, "fp8": BF, "f32": FF}[kind], fp8=kind == "fp8", mask=False)
+    check_tree(c, *run_tree(c))
+    out, lse = run_tree(c, softmax_scale=0.31)
+    check_tree(c, out, lse, scale=float(np.float32(0.31)))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp8", "f32"])
+def test_tree_attention_empty_rows_and_rows_behind(kind):
+    """Mask rows of zeros (over no committed token: nothing is seen), mask words beyond the new tokens, untouched rows behind."""
+    c = tree_case(8, [(0, 6), (40, 5), (0, 40)], 8, 2, 128, FF if kind == "f32" else BF, fp8=kind == "fp8")
+    mask = c["mask"].clone()
+    mask[2] = 0
+    mask[7] = 0
+    mask[11:51] = 0
+    mask[30, 1] = -1                           # sees tokens 32 .. 39 and bits past the last one
+    c["mask"] = mask
+    c["sees"][0][2] = False
+    c["sees"][1][1] = False
+    c["sees"][2][:] = False
+    c["sees"][2][19, 32:] = True
+    check_tree(c, *run_tree(c))
+    T = c["T"]
+    import paper_2410_03960_b200 as P
+    wide = dict(c, T=T + 3, q=torch.cat([c["q"], c["q"][:3]]).contiguous())
+    out = torch.full((T + 3, 8, 128), 5.0, dtype=c["dt"], device="cuda")
+    o, lse = run_tree(dict(wide, mask=torch.cat([mask, mask[:3]])), out=out)
+    check_tree(c, o[:T].contiguous(), lse[:T].contiguous())
+    assert (o[T:] == 5).all() and (lse[T:] == 77).all()
+    P.op_status()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16", "fp8", "f32"])
+@pytest.mark.parametrize("lens", [[(250, 6), (0, 9)], [(128, 20)], [(3, 120)]], ids=str)
+def test_tree_attention_ignores_what_is_not_seen(kind, lens):
+    """NaN and infinities in cache rows behind a sequence's last token, in free pages, and in a drafted token's K and V that others do
+    not see: the others' results keep their bits."""
+    c = tree_case(21, lens, 8, 2, 128, {"bf16": BF, "f16": HF, "fp8": BF, "f32": FF}[kind], fp8=kind == "fp8")
+    # the first sequence's token 1 is seen by nobody but itself
+    c["mask"][:, 0] &= ~2
+    c["mask"][1, 0] |= 2
+    for s in c["sees"]:
+        s[:, 1] = False
+    c["sees"][0][1, 1] = True
+    c["mask"][c["cu"][0] + 1, 0] |= 2
+    if len(lens) > 1:
+        assert not (c["mask"][c["cu"][1]:, 0] & 2).any()
+    clean, clean_lse = run_tree(c)
+    check_tree(c, clean, clean_lse)
+    used = np.concatenate(c["rows"])
+    free = np.setdiff1d(np.arange(c["k"].shape[0]), used)
+    hidden = int(c["rows"][0][lens[0][0] + 1])
+    d = dict(c, k=c["k"].clone(), v=c["v"].clone())
+    if kind == "fp8":
+        d["ks"], d["vs"] = c["ks"].clone(), c["vs"].clone()
+        for t in (d["k"], d["v"]):
+            t[free] = 0x7F                     # the code that stands for no number
+            t[hidden] = 0x7E
+        for t in (d["ks"], d["vs"]):
+            t[free] = float("nan")
+            t[hidden] = float("inf")
+    else:
+        for t in (d["k"], d["v"]):
+            t[free] = float("nan")
+            t[hidden] = float("inf")
+            t[hidden, 0, ::3] = float("nan")
+    out, lse = run_tree(d)
+    others = [t for t in range(c["T"]) if t != 1]
+    assert torch.equal(out[others], clean[others]) and torch.equal(lse[others], clean_lse[others])
+    assert not torch.isfinite(out[1].float()).all()          # and the one that sees it does not hide it
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp8", "f32"])
+def test_tree_attention_large_scores(kind):
+    """Scores of some hundreds, rising along the keys (every tile moves the reference maximum) and falling."""
+    for sign in (1.0, -1.0):
+        c = tree_case(31, [(900, 4)], 4, 2, 128, FF if kind == "f32" else BF, fp8=kind == "fp8")
+        c["q"] = torch.ones_like(c["q"])
+        ramp = torch.linspace(-3, 3, 904, device="cuda") * sign * 10
+        rows = torch.as_tensor(c["rows"][0], device="cuda")
+        if kind == "fp8":
+            c["k"][rows] = 0x38                # 1.0
+            c["ks"][rows] = ramp.abs() + 1e-3
+            neg = rows[ramp < 0]
+            c["k"][neg] = 0xB8
+        else:
+            c["k"][rows] = ramp[:, None, None].to(c["dt"]).expand(-1, 2, 128)
+        check_tree(c, *run_tree(c))
+
+
+def test_tree_attention_reports_lengths_and_pages():
+    """Pages outside the cache read as zero rows; lengths beyond what the call promises are cut and reported."""
+    import paper_2410_03960_b200 as P
+    for kind in (BF, FF):
+        c = tree_case(41, [(300, 4)], 4, 2, 128, kind)
+        c["table"][0, 1] = 10 ** 6
+        c["rows"][0][128:256] = -1
+        check_tree(c, *run_tree(c))
+        c["table"][0, 1] = -5
+        check_tree(c, *run_tree(c))
+        P.op_status()
+        run_tree(dict(c, max_new=3))
+        with pytest.raises(P.SwiftKVError) as e:
+            P.op_status()
+        assert e.value.code == -6
+        run_tree(dict(c, max_kv=200))
+        with pytest.raises(P.SwiftKVError):
+            P.op_status()
+
+
+def test_tree_attention_one_token_equals_tail_attention():
+    """One new token per sequence is the single-query attention of the last-token path."""
+    import paper_2410_03960_b200 as P
+    lens = [(699, 1), (128, 1), (2999, 1)]
+    c = tree_case(51, lens, 32, 8, 128, BF, paged=False)
+    k = torch.cat([c["k"][torch.as_tensor(r, device="cuda")] for r in c["rows"]]).contiguous()
+    v = torch.cat([c["v"][torch.as_tensor(r, device="cuda")] for r in c["rows"]]).contiguous()
+    ref = P.tail_attention(c["q"].float().contiguous(), k, v, [p + 1 for p, _ in lens]).view(3, 32, 128)
+    out, _ = run_tree(c)
+    # both round probabilities: 2^-9 each at most, on outputs of sum p |v| <= max |v| (about 4.5)
+    assert (out.float() - ref).abs().max() <= 2.0 ** -8 * float(v.float().abs().max())
+
+
+def test_tree_attention_beyond_32_bit_offsets():
+    """Cache planes of more than 2^32 bytes / 2^31 elements: rows at their far end."""
+    import paper_2410_03960_b200 as P
+    n_kv, hd = 8, 128
+    rows = (1 << 31) // (n_kv * hd) + 4096                    # elements beyond 2^31, 4.3 GB per plane
+    if torch.cuda.mem_get_info()[0] < 14 << 30:
+        pytest.skip("needs 14 GB")
+    k, v = (torch.zeros((rows, n_kv, hd), dtype=BF, device="cuda") for _ in range(2))
+    c = tree_case(61, [(600, 5)], 16, n_kv, hd, BF, paged=False)
+    first = rows - 700
+    src = torch.as_tensor(c["rows"][0], device="cuda")
+    k[first: first + 605], v[first: first + 605] = c["k"][src], c["v"][src]
+    out, lse = run_tree(dict(c, k=k, v=v, row0=i32([first])))
+    check_tree(c, out, lse)
+    P.op_status()
+
+
+# --------------------------------------------------------------------------------------------------- token_logprobs
+def lp_case(rows, vocab, dt, seed, pad=0, std=2.5):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    x = torch.empty((rows, vocab + pad), dtype=dt, device="cuda").normal_(0, std, generator=g)[:, :vocab]
+    t = torch.randint(0, vocab, (rows,), generator=g, device="cuda", dtype=torch.int32)
+    return g, x, t
+
+
+def check_lp(x, t, temperature, k, got):
+    """lse, logprob, entropy in fp32: exponents (z - m) carry 2 roundings of their own size, so p is good to 2^-22 (1 + range) with range
+    the spread of the logits that matter (p > 2^-24: about 17 + 1); log2 is good to 2^-21 absolute, the sums to (vocab / 4096 + 32)
+    2^-24 relative; adding m / T rounds once at its size."""
+    xn = f64(x)
+    with np.errstate(all="ignore"):
+        want = R.token_logprobs(xn, np.maximum(t.cpu().numpy(), -1), temperature, k)
+    rel = 20 * 2.0 ** -22 + (xn.shape[1] / 4096 + 32) * 2.0 ** -24 + 2.0 ** -21
+    for name in ("lse", "logprob", "entropy") + (("top_logprobs",) if k else ()):
+        a, b = f64(got[name]), want[name]
+        fin = np.isfinite(b)
+        assert np.array_equal(fin, np.isfinite(a)), name
+        scale = np.where(np.isfinite(want["lse"]), np.abs(want["lse"]), 0) * 2.0 ** -22
+        tol = rel * (1 + np.abs(np.where(fin, b, 0)) * 2.0 ** -1 * (name == "entropy")) + (scale if a.ndim == 1 else scale[:, None]) + 2.0 ** -21 * np.abs(np.where(fin, b, 0))
+        assert (np.abs(np.where(fin, a - np.where(fin, b, 0), 0)) <= tol).all(), (name, np.nanmax(np.abs(a - b)))
+    if k:
+        assert np.array_equal(got["top_ids"].cpu().numpy(), want["top_ids"])
+
+
+@pytest.mark.parametrize("rows,vocab,pad", [(1, 1, 0), (1, 5, 0), (3, 17, 2), (2, 1000, 1), (5, 4097, 0), (9, 32000, 0), (1, 128256, 0), (200, 50001, 0), (3, 160001, 63), (40, 8191, 1)])
+@pytest.mark.parametrize("dt", [FF, BF, HF])
+@pytest.mark.parametrize("k,temperature", [(0, 1.0), (1, 0.7), (5, 1.0), (20, 2.0), (32, 1.0)])
+def test_token_logprobs(rows, vocab, pad, dt, k, temperature):
+    import paper_2410_03960_b200 as P
+    _, x, t = lp_case(rows, vocab, dt, rows + vocab, pad)
+    t[rows // 2] = -1
+    k = min(k, vocab)
+    got = P.token_logprobs(x, t, top_k=k, temperature=temperature)
+    P.op_status()
+    check_lp(x, t, float(np.float32(temperature)), k, got)
+
+
+@pytest.mark.parametrize("dt", [FF, BF])
+@pytest.mark.parametrize("split", [True, False])
+def test_token_logprobs_ties_and_orders(dt, split):
+    """Equal logits keep the lowest index first; rising, falling and constant rows; zeros of both signs are equal."""
+    import paper_2410_03960_b200 as P
+    rows, vocab = (6, 40000) if split else (6 * 160, 9000)
+    x = torch.zeros((rows, vocab), dtype=dt, device="cuda")
+    i = torch.arange(vocab, device="cuda")
+    x[1::6] = (i / 1000).to(dt)
+    x[2::6] = (-i / 1000).to(dt)
+    x[3::6] = torch.where(i % 2 == 0, 0.0, -0.0).to(dt)
+    x[4::6] = ((i * 7919) % 13).to(dt)
+    x[5::6] = torch.where(i >= vocab - 40, 3.0, 1.0).to(dt)
+    t = torch.full((rows,), vocab - 1, dtype=torch.int32, device="cuda")
+    for k in (1, 7, 32):
+        check_lp(x, t, 1.0, k, P.token_logprobs(x, t, top_k=k))
+
+
+def test_token_logprobs_masked_and_peaked():
+    """Logits of -inf, of the type's lowest value, of some thousands; all mass on one token; rows without any finite logit."""
+    import paper_2410_03960_b200 as P
+    _, x, t = lp_case(12, 5000, FF, 4)
+    x[0, 10:] = -math.inf
+    x[1, :4990] = torch.finfo(FF).min
+    x[2] *= 1000
+    x[3, 77] = 60.0
+    x[4, :] = -math.inf
+    x[4, 4321] = -5.0
+    x[5, :] = torch.finfo(FF).min
+    x[6, 0] = -math.inf
+    x[7, 1:] = -math.inf
+    t[3], t[4], t[6], t[7] = 77, 4321, 0, 0
+    got = P.token_logprobs(x[:4], t[:4], top_k=5)
+    check_lp(x[:4], t[:4], 1.0, 5, {k: v for k, v in got.items()})
+    got = P.token_logprobs(x[4:12].contiguous(), t[4:12], top_k=5)
+    check_lp(x[4:12], t[4:12], 1.0, 5, got)
+    y = x[8:11].clone()
+    y[0] = -math.inf
+    y[1, 9] = math.nan
+    y[2, 8] = math.inf
+    got = P.token_logprobs(y, t[:3], top_k=2)
+    assert got["lse"][0] == -math.inf and torch.isnan(got["entropy"]).all() and torch.isnan(got["logprob"]).all()
+    for i, at in ((0, 0), (1, 4999), (2, 2500)):             # a NaN among masked logits, wherever it is met
+        z = torch.full((1, 5000), -math.inf if i else torch.finfo(FF).min, device="cuda")
+        z[0, at] = math.nan
+        z[0, 10:20] = 1.0
+        assert all(torch.isnan(v).all() for v in P.token_logprobs(z, t[:1] * 0 + 12).values())
+    assert torch.isnan(got["lse"][1:]).all() and got["top_ids"][1, 0] == 9 and got["top_ids"][2, 0] == 8 and got["top_ids"][0].tolist() == [0, 1]
+    P.op_status()
+
+
+def test_token_logprobs_reports_bad_targets():
+    import paper_2410_03960_b200 as P
+    _, x, t = lp_case(3, 100, BF, 5)
+    t[1] = 100
+    got = P.token_logprobs(x, t)
+    assert got["logprob"][1] == 0
+    with pytest.raises(P.SwiftKVError) as e:
+        P.op_status()
+    assert e.value.code == -6
+    none = P.token_logprobs(x)
+    assert (none["logprob"] == 0).all() and torch.equal(none["lse"], got["lse"])
+
+
+@pytest.mark.parametrize("rows,vocab,pad,out_pad", [(1, 1, 0, 0), (3, 17, 2, 0), (2, 1000, 1, 3), (5, 4097, 0, 0), (4, 32000, 8, 0), (7, 9001, 0, 4), (300, 1009, 2, 0)])
+@pytest.mark.parametrize("dt", [FF, BF, HF])
+@pytest.mark.parametrize("entropy", [True, False])
+def test_token_logprobs_gradient(rows, vocab, pad, out_pad, dt, entropy):
+    """|d - want| <= u |want| + e (|g_lp| p + |g_H| p (|log p| + H)) / T, e the relative error of p: the exponent's, which is its size (z and lse
+    up to about 20: 2^-20) plus exp2's 2^-22, and lse's and H's own rounding to fp32."""
+    import paper_2410_03960_b200 as P
+    g, x, t = lp_case(rows, vocab, dt, rows * 3 + vocab, pad)
+    t[0] = -1
+    T = 0.7
+    fwd = P.token_logprobs(x, t, temperature=T)
+    g_lp, g_h = (torch.randn(rows, generator=g, device="cuda") for _ in range(2))
+    g_h = g_h if entropy else None
+    out = torch.full((rows, vocab + out_pad), 3.0, dtype=dt, device="cuda")
+    got = P.token_logprobs_bwd(x, t, fwd["lse"], fwd["entropy"] if entropy else None, g_lp, g_h, temperature=T, out=out[:, :vocab])
+    P.op_status()
+    assert (out[:, vocab:] == 3).all()
+    xn, tn, Tn = f64(x), t.cpu().numpy(), float(np.float32(T))
+    want = R.token_logprobs_bwd(xn, tn, Tn, f64(g_lp), None if g_h is None else f64(g_h))
+    w = R.token_logprobs(xn, tn, Tn, 0)
+    logp = xn / Tn - w["lse"][:, None]
+    p = np.exp(logp)
+    mag = np.abs(f64(g_lp))[:, None] * (p + (np.arange(vocab) == tn[:, None]))
+    if g_h is not None:
+        mag = mag + np.abs(f64(g_h))[:, None] * p * (1 + np.abs(logp) + w["entropy"][:, None])
+    assert (np.abs(f64(got) - want) <= u_of(dt) * np.abs(want) + 2.0 ** -18 * mag / Tn + tiny_of(dt)).all()
+    if pad == 0 and out_pad == 0:
+        y = x.clone()
+        again = P.token_logprobs_bwd(y, t, fwd["lse"], fwd["entropy"], g_lp, g_h, temperature=T, out=y)
+        assert again.data_ptr() == y.data_ptr() and torch.equal(again, got)
+
+
+def test_token_logprobs_gradient_against_differences():
+    """Directional derivatives of the 64-bit forward formula (h = 1e-4: error about 1e-7 of the terms)."""
+    import paper_2410_03960_b200 as P
+    g, x, t = lp_case(4, 300, FF, 8)
+    t[2] = -1
+    fwd = P.token_logprobs(x, t, temperature=2.0)
+    g_lp, g_h = (torch.randn(4, generator=g, device="cuda") for _ in range(2))
+    d = f64(P.token_logprobs_bwd(x, t, fwd["lse"], fwd["entropy"], g_lp, g_h, temperature=2.0))
+    xn, tn = f64(x), t.cpu().numpy()
+
+    def f(y):
+        w = R.token_logprobs(y, tn, 2.0, 0)
+        return float((w["logprob"] * f64(g_lp)).sum() + (w["entropy"] * f64(g_h)).sum())
+
+    rng = np.random.default_rng(1)
+    for _ in range(4):
+        e = rng.standard_normal(xn.shape)
+        num = (f(xn + 1e-4 * e) - f(xn - 1e-4 * e)) / 2e-4
+        assert abs(num - (d * e).sum()) <= (2.0 ** -17 + 1e-6) * np.abs(d * e).sum() + 1e-9
+
+
+def test_token_logprobs_gradient_of_masked_logits():
+    import paper_2410_03960_b200 as P
+    g, x, t = lp_case(2, 600, BF, 9)
+    x[:, 100:300] = -math.inf
+    x[:, 300:400] = torch.finfo(BF).min
+    t[:] = 5
+    fwd = P.token_logprobs(x, t)
+    big = torch.full((2,), 1e9, device="cuda")
+    d = P.token_logprobs_bwd(x, t, fwd["lse"], fwd["entropy"], big, big)
+    assert torch.isfinite(d.float()).all() and (d[:, 100:400] == 0).all()
+
+
+# -------------------------------------------------------------------------------------------------------- together
+class Step:
+    """One layer's verification step over a paged cache, as a server would run it: plan, norm + rotate + store, attend, score."""
+
+    def __init__(self, seed, lens, fp8=False, n_q=8, n_kv=2, hd=128, vocab=5000):
+        import paper_2410_03960_b200 as P
+        self.P, self.fp8, self.n_q, self.n_kv, self.hd = P, fp8, n_q, n_kv, hd
+        rng = np.random.default_rng(seed)
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        self.past, self.new = [p for p, _ in lens], [n for _, n in lens]
+        T = self.T = sum(self.new)
+        owned = [-(-p // 128) for p in self.past]
+        pages = rng.permutation(sum(owned) + 20)
+        blocks = max(-(-(p + n) // 128) for p, n in lens) + 1
+        table, at = np.full((len(lens), blocks), -1), 0
+        for b, o in enumerate(owned):
+            table[b, :o] = pages[at: at + o]
+            at += o
+        self.host = (owned, table, pages[at:], len(pages) - at, blocks)
+        self.d = dict(past=i32(self.past), new=i32(self.new), owned=i32(owned), table=i32(table), free=i32(pages[at:]), n_free=i32([len(pages) - at]))
+        rows = len(pages) * 128
+        make = lambda *s: torch.randn(s, generator=g, device="cuda")  # noqa: E731
+        if fp8:
+            self.k, self.v = (make(rows, n_kv, hd).mul(100).clamp(-448, 448).to(torch.float8_e4m3fn).view(torch.uint8) for _ in range(2))
+            self.ks, self.vs = (torch.rand(rows, generator=g, device="cuda") / 100 + 0.005 for _ in range(2))
+        else:
+            self.k, self.v, self.ks, self.vs = make(rows, n_kv, hd).to(BF), make(rows, n_kv, hd).to(BF), None, None
+        self.qkv = make(T, (n_q + 2 * n_kv) * hd).to(BF)
+        self.qg, self.kg = (1 + 0.2 * make(hd)).to(BF), (1 + 0.2 * make(hd)).to(BF)
+        self.cos, self.sin = P.rope_table(4096, hd, THETA)
+        words = -(-max(self.new) // 32)
+        trees = [random_tree(rng, n, words) for n in self.new]
+        self.mask, self.sees = i32(np.concatenate([m for m, _ in trees])), [s for _, s in trees]
+        self.logits = make(T, vocab).to(BF)
+        self.targets = torch.randint(0, vocab, (T,), generator=g, device="cuda", dtype=torch.int32)
+        self.before = (self.k.clone(), self.v.clone(), None if not fp8 else self.ks.clone(), None if not fp8 else self.vs.clone())
+
+    def run(self, stream=None):
+        P, d, n_q, n_kv, hd = self.P, self.d, self.n_q, self.n_kv, self.hd
+        plan = P.plan_pages(d["past"], d["new"], d["owned"], d["table"], d["free"], d["n_free"], max_tokens=self.T, stream=stream)
+        q, k, v = (self.qkv[:, a * hd: (a + n) * hd].view(self.T, n, hd) for a, n in ((0, n_q), (n_q, n_kv), (n_q + n_kv, n_kv)))
+        q = P.qk_norm_rope(q, k, v, plan["positions"], self.cos, self.sin, q_gain=self.qg, k_gain=self.kg, k_cache=self.k, v_cache=self.v, k_scale=self.ks,
+                           v_scale=self.vs, slot_map=plan["slot_map"], stream=stream)
+        lse = torch.empty((self.T, n_q), device="cuda")
+        o = P.tree_attention(q, self.k, self.v, d["past"], plan["cu_new"], max(self.new), max(a + b for a, b in zip(self.past, self.new)),
+                             block_table=plan["block_table"], tree_mask=self.mask, k_scale=self.ks, v_scale=self.vs, lse=lse, stream=stream)
+        return plan, q, o, lse, P.token_logprobs(self.logits, self.targets, top_k=4, stream=stream)
+
+    def check(self, got):
+        """The plan exactly; each later operator against its reference on what the ones before it gave."""
+        plan, q, o, lse, lp = got
+        owned, table, free, n_free, blocks = self.host
+        want = R.plan(self.past, self.new, owned, table, free, n_free, blocks)
+        for name, x in want.items():
+            assert np.array_equal(plan[name].cpu().numpy(), x), name
+        n_q, n_kv, hd, T = self.n_q, self.n_kv, self.hd, self.T
+        x = f64(self.qkv).reshape(T, n_q + 2 * n_kv, hd)
+        p = want["positions"]
+        wq = R.rotate(R.head_norm(x[:, :n_q], f64(self.qg), EPS), p, THETA)
+        assert (np.abs(f64(q) - wq) <= rope_bound(x[:, :n_q], f64(self.qg), p, 2.0 ** -8, hd, wq)).all()
+        slots = want["slot_map"]
+        wk = R.rotate(R.head_norm(x[:, n_q: n_q + n_kv], f64(self.kg), EPS), p, THETA)
+        if not self.fp8:
+            assert (np.abs(f64(self.k)[slots] - wk) <= rope_bound(x[:, n_q: n_q + n_kv], f64(self.kg), p, 2.0 ** -8, hd, wk)).all()
+            assert np.array_equal(f64(self.v)[slots], x[:, n_q + n_kv:])
+        left = np.setdiff1d(np.arange(self.k.shape[0]), slots)
+        assert torch.equal(self.k[left], self.before[0][left]) and torch.equal(self.v[left], self.before[1][left])
+        rows = [want["block_table"][b][np.arange(a + n) // 128] * 128 + np.arange(a + n) % 128 for b, (a, n) in enumerate(zip(self.past, self.new))]
+        c = dict(q=q, k=self.k, v=self.v, ks=self.ks, vs=self.vs, past=self.past, cu=want["cu_new"].astype(int), rows=rows, sees=self.sees, dt=BF, fp8=self.fp8, hd=hd,
+                 max_kv=max(a + b for a, b in zip(self.past, self.new)))
+        check_tree(c, o, lse)
+        check_lp(self.logits, self.targets, 1.0, 4, lp)
+
+
+LENS_STEP = [(300, 9), (0, 5), (127, 1), (128, 33), (1000, 12)]
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+def test_a_verification_step(fp8):
+    s = Step(71, LENS_STEP, fp8)
+    s.check(s.run())
+    s.P.op_status()
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+def test_a_verification_step_on_another_stream_and_two_at_once(fp8):
+    a, b = Step(72, LENS_STEP, fp8), Step(73, LENS_STEP[::-1], fp8)
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(3):
+        for s in (s1, s2):
+            s.wait_stream(torch.cuda.current_stream())
+        ga, gb = a.run(s1), b.run(s2)
+        s1.synchronize()
+        s2.synchronize()
+    a.check(ga)
+    b.check(gb)
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+def test_a_verification_step_captured_and_replayed(fp8):
+    """Two graphs over the same kernels, replayed in turn and side by side, with inputs changed in between."""
+    a, b = Step(74, LENS_STEP, fp8), Step(75, LENS_STEP[::-1], fp8)
+    a.run(), b.run()
+    torch.cuda.synchronize()
+    graphs, got = [], []
+    for s in (a, b):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            got.append(s.run())
+        graphs.append(g)
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    for k in range(3):
+        for s in (a, b):
+            s.qkv.mul_(-1.25 if k else 1.0)
+            s.logits.add_(0.5)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(s1):
+            graphs[0].replay()
+        with torch.cuda.stream(s2):
+            graphs[1].replay()
+        torch.cuda.synchronize()
+        a.check(got[0])
+        b.check(got[1])
+
+
+def test_the_gradients_captured_and_replayed():
+    import paper_2410_03960_b200 as P
+    g, q, k, v, pos, (qg, kg) = rope_inputs(60, 8, 2, 128, BF, 81)
+    dq, dk = (torch.randn((60, n, 128), generator=g, device="cuda").to(BF) for n in (8, 2))
+    cos, sin = P.rope_table(131072, 128, THETA)
+    _, x, t = lp_case(5, 3001, BF, 82)
+    gl = torch.randn(5, generator=g, device="cuda")
+
+    def both():
+        f = P.token_logprobs(x, t)
+        return P.qk_norm_rope_bwd(dq, dk, q, k, pos, cos, sin, q_gain=qg, k_gain=kg) + (P.token_logprobs_bwd(x, t, f["lse"], f["entropy"], gl, gl),)
+
+    both()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = both()
+    for _ in range(2):
+        dq.mul_(0.5)
+        x.add_(1.0)
+        graph.replay()
+        for a, b in zip(got, both()):
+            assert torch.equal(a, b)
