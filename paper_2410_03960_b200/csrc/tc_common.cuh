@@ -283,9 +283,10 @@ __device__ __forceinline__ uint32_t pack_act(float lo, float hi, bool f16) {
 
 // ---- host: tensor maps ---------------------------------------------------------------------------------------
 // Row-major bf16 matrix [rows, cols] (row stride ld elements); box = box_cols x box_rows, 128-byte swizzle
-// (box_cols must be 64), out-of-range rows/cols read as zero.  Returns 0 on success.
+// (box_cols must be 64), out-of-range rows/cols read as zero; swizzle false: the box's rows packed as they are.
+// Returns 0 on success.
 int make_tmap_2d_bf16(CUtensorMap *out, const void *base, uint64_t rows, uint64_t cols, uint64_t ld,
-                      uint32_t box_rows, uint32_t box_cols);
+                      uint32_t box_rows, uint32_t box_cols, bool swizzle = true);
 // bf16 tensor [d2][d1][d0] with element strides (s2, s1, 1); box (b0, b1, b2), 128-byte swizzle.
 int make_tmap_3d_bf16(CUtensorMap *out, const void *base, uint64_t d0, uint64_t d1, uint64_t d2, uint64_t s1,
                       uint64_t s2, uint32_t b0, uint32_t b1, uint32_t b2);

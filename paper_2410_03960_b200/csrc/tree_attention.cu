@@ -31,12 +31,12 @@ struct TreeArgs {
 };
 
 // lengths beyond what the host promised (max_new, max_kv, total_new) are cut, so that no loop outgrows them, and reported
-__device__ __forceinline__ void tree_lengths(const TreeArgs &a, int b, int &tok0, int &n, int &past) {
+__device__ __forceinline__ void tree_lengths(const TreeArgs &a, int b, int &tok0, int &n, int &past, bool report) {
   const int c0 = a.cu[b], c1 = a.cu[b + 1], p = a.past[b];
   tok0 = min(max(0, c0), a.total_new);
   n = min(min(min(max(0, c1 - c0), a.max_new), a.total_new - tok0), a.max_kv);
   past = min(max(0, p), a.max_kv - n);
-  if ((n != c1 - c0 || past != p) && threadIdx.x == 0) atomicOr(a.status, STATUS_BAD_TOKEN);
+  if (report && (n != c1 - c0 || past != p)) atomicOr(a.status, STATUS_BAD_TOKEN);
 }
 // cache row of key p, -1 where the tables lead outside the cache (such a row reads as zeros)
 __device__ __forceinline__ int tree_row(const TreeArgs &a, int b, int p) {
@@ -90,7 +90,7 @@ __global__ void __launch_bounds__(TS_THREADS) tree_attention_simt_kernel(TreeArg
   const int chunk = u % row_chunks; u /= row_chunks;
   const int kvh = u % a.n_kv, b = u / a.n_kv;
   int tok0, n, past;
-  tree_lengths(a, b, tok0, n, past);
+  tree_lengths(a, b, tok0, n, past, threadIdx.x == 0);
   const int rows = n * rep, r0 = chunk * TS_ROWS, kv = past + n;
   if (r0 >= rows) return;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -221,6 +221,808 @@ size_t simt_scratch(int total_new, int max_kv, int n_q, int hd) {
   return splits > 1 ? (size_t)total_new * n_q * splits * (hd + 2) * sizeof(float) : 0;
 }
 
+// ---------------------------------------------------------------------------------------------------------
+// Tensor-core form (head_dim 64 / 128, 16-bit queries, cache of their type or FP8).
+//
+// A query tile is 128 rows = (128 / rep new tokens) x (the rep query heads of one KV head), so that a K / V tile of 128 keys
+// -- exactly one page -- is read once for all of them.  tcgen05: S = Q K^T into tensor memory, a row per softmax thread,
+// P back over S in 16 bits, O += P V with P read from tensor memory (P bf16; f16 with f16 caches).  Two streams of softmax
+// warps keep the tensor pipe and the loads busy while the other one exponentiates:
+//   W = 2: stream w owns query tile w of a pair, both use every K / V tile (up to 256 rows a pass over the cache);
+//   W = 1: stream w owns the key tiles of parity w of ONE query tile, and the two accumulators are joined at the end.
+// Sums and maxima are fp32; the reference maximum moves only when a row outgrows it by 2^8 (O is then rescaled).
+//
+// Work split: the (sequence, tile group, KV head, key tile) units of a call, in this order, are cut into equal contiguous
+// ranges, one per CTA (one CTA per SM).  The lengths live on the device, so every CTA sums them up for itself.  A range that
+// starts or ends inside a (sequence, group, head) leaves an unnormalised partial result in `scratch` (at most two per CTA),
+// and a second kernel joins those in the order of the keys: deterministic, and balanced for any mix of lengths.
+//
+// FP8 rows: TMA brings the codes, four warps widen them to the 16-bit type exactly (every e4m3 number is one) and the fp32
+// scales of the rows enter after Q K^T (K) and into P before its rounding (V).
+//
+// What is not seen must not matter: keys behind the sequence and unseen drafts get S = -inf, and the V rows of the last
+// tiles are cleaned in shared memory first (0 * NaN is NaN): rows behind the sequence become zeros, and a drafted token's V row that
+// holds infinities or NaN is zeroed and handed to the rows that do see it in the epilogue.
+// ---------------------------------------------------------------------------------------------------------
+constexpr int TT_KEYS = 128;
+constexpr float TT_RESCALE = 8.0f;       // in log2 units
+
+template <int HD, int W, bool FP8>
+struct TreeLayout {
+  static constexpr int TILE = 128 * HD * 2, CHUNK = 128 * 128, CHUNKS = HD / 64;
+  static constexpr int CODE_TILE = 128 * HD;
+  static constexpr int KS = FP8 ? 1 : (HD == 64 ? 4 : 2), VS = FP8 ? 2 : (HD == 64 ? 4 : (W == 2 ? 2 : 3)), CS = FP8 ? 5 : 0;
+  static constexpr int Q = 0, K = W * TILE, V = K + KS * TILE, C = V + VS * TILE, SC = C + CS * CODE_TILE;
+  static constexpr int ML = SC + (FP8 ? 4 * 2 * 128 * 4 : 0);       // scales: 4 tiles x (K, V) x 128
+  static constexpr int BAR = ML + 2 * 2 * 128 * 8;                  // (m, l) of both streams, two items
+  static constexpr int BYTES = BAR + 512 + 1024;
+  static constexpr int WARPS = 11 + (FP8 ? 4 : 0);
+  static constexpr int THREADS = WARPS * 32;
+};
+
+struct TreeTcArgs {
+  TreeArgs a;
+  int npt;               // new tokens per query tile
+  int slot_rows;         // rows of a partial result in scratch
+  float scale_log2;
+  int store32;
+};
+
+__device__ __forceinline__ bool tt_wait(uint32_t bar, uint32_t parity, volatile int *abort_flag, unsigned int *status) {
+  if (tc::mbar_try_wait(bar, parity)) return true;
+  const long long t0 = clock64();
+  for (unsigned spins = 1;; ++spins) {
+    if (tc::mbar_try_wait(bar, parity)) return true;
+    if ((spins & 31u) == 0u) {
+      if (*abort_flag) return false;
+      if (clock64() - t0 > tc::WAIT_LIMIT_CLOCKS) {
+        *abort_flag = 1;
+        atomicOr(status, STATUS_TIMEOUT);
+        return false;
+      }
+    }
+  }
+}
+__device__ __forceinline__ float tt_exp2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// units of a sequence: key tiles x KV heads x groups of W query tiles
+struct SeqShape { int tok0, n, past, tiles, groups; };
+__device__ __forceinline__ SeqShape seq_shape(const TreeArgs &a, int b, int group_tokens) {
+  SeqShape s;
+  tree_lengths(a, b, s.tok0, s.n, s.past, false);
+  s.tiles = (s.past + s.n + TT_KEYS - 1) / TT_KEYS;
+  s.groups = (s.n + group_tokens - 1) / group_tokens;
+  return s;
+}
+// a CTA's walk over its units, one (sequence, group, head) piece after the other; every role keeps its own
+struct Pieces {
+  int b, g, h, kt0, kt1, left, group_tokens;
+  SeqShape s;
+  __device__ __forceinline__ void begin(const TreeArgs &a, int b0, int within, int units, int gt) {
+    group_tokens = gt;
+    b = b0;
+    s = seq_shape(a, b, gt);
+    left = units;
+    kt0 = within % s.tiles;
+    const int item = within / s.tiles;
+    h = item % a.n_kv;
+    g = item / a.n_kv;
+    kt1 = min(s.tiles, kt0 + left);
+  }
+  __device__ __forceinline__ bool next(const TreeArgs &a) {
+    left -= kt1 - kt0;
+    if (left <= 0) return false;
+    if (++h == a.n_kv) {
+      h = 0;
+      if (++g >= s.groups) {
+        g = 0;
+        do { s = seq_shape(a, ++b, group_tokens); } while (s.groups == 0);
+      }
+    }
+    kt0 = 0;
+    kt1 = min(s.tiles, left);
+    return true;
+  }
+  __device__ __forceinline__ bool whole() const { return kt0 == 0 && kt1 == s.tiles; }
+};
+__device__ __forceinline__ int units_of(const TreeArgs &a, const SeqShape &s) { return s.tiles * s.groups * a.n_kv; }
+
+// 32 visibility bits of keys j0 .. j0 + 31, counted from the first new token (negative: committed), for new token i
+__device__ __forceinline__ uint32_t mask_word(const TreeArgs &a, int t, int i, int n, int w) {
+  const int first = 32 * w;
+  if (first >= n) return 0u;
+  uint32_t m;
+  if (a.mask) m = w < a.mask_words ? (uint32_t)a.mask[(size_t)t * a.mask_words + w] : 0u;
+  else m = i >= first + 31 ? 0xffffffffu : i < first ? 0u : (2u << (i - first)) - 1u;
+  return n - first >= 32 ? m : m & ((1u << (n - first)) - 1u);
+}
+__device__ __forceinline__ uint32_t sees_word(const TreeArgs &a, int t, int i, int n, int j0) {
+  if (j0 <= -32) return 0xffffffffu;
+  if (j0 < 0) return (mask_word(a, t, i, n, 0) << -j0) | ((1u << -j0) - 1u);
+  const uint32_t lo = mask_word(a, t, i, n, j0 >> 5);
+  return (j0 & 31) ? __funnelshift_r(lo, mask_word(a, t, i, n, (j0 >> 5) + 1), j0 & 31) : lo;
+}
+
+// e4m3 codes as the 16-bit type, exactly: the code's exponent and mantissa bits are those of the wider type with another bias
+__device__ __forceinline__ void widen4(uint32_t codes, uint32_t &lo, uint32_t &hi, bool half) {
+  const uint32_t a = __byte_perm(codes, 0u, 0x1404), b = __byte_perm(codes, 0u, 0x3424);      // two codes in the upper bytes of two halves
+  if (half) {
+    const uint32_t x = (a & 0x80008000u) | ((a >> 1) & 0x3f803f80u), y = (b & 0x80008000u) | ((b >> 1) & 0x3f803f80u);
+    const __half2 f = __float2half2_rn(256.f);
+    const __half2 u = __hmul2(*reinterpret_cast<const __half2 *>(&x), f), v = __hmul2(*reinterpret_cast<const __half2 *>(&y), f);
+    lo = *reinterpret_cast<const uint32_t *>(&u);
+    hi = *reinterpret_cast<const uint32_t *>(&v);
+  } else {
+    const uint32_t x = (a & 0x80008000u) | ((a >> 4) & 0x07f007f0u), y = (b & 0x80008000u) | ((b >> 4) & 0x07f007f0u);
+    const __nv_bfloat162 f = __float2bfloat162_rn(1.329227995784916e36f);      // 2^120
+    const __nv_bfloat162 u = __hmul2(*reinterpret_cast<const __nv_bfloat162 *>(&x), f), v = __hmul2(*reinterpret_cast<const __nv_bfloat162 *>(&y), f);
+    lo = *reinterpret_cast<const uint32_t *>(&u);
+    hi = *reinterpret_cast<const uint32_t *>(&v);
+  }
+}
+
+// first cache row of key tile j (a row outside the cache: the tile reads as zeros)
+__device__ __forceinline__ int tile_row(const TreeArgs &a, int b, int j) {
+  if (a.blk) {
+    if (j >= a.max_blocks) return a.cache_rows;
+    const int page = a.blk[(size_t)b * a.max_blocks + j];
+    return page < 0 || page > a.cache_rows / PAGE_ROWS ? a.cache_rows : page * PAGE_ROWS;
+  }
+  const long long r = (long long)a.row0[b] + (long long)j * TT_KEYS;
+  return r < -TT_KEYS || r > a.cache_rows ? a.cache_rows : (int)r;
+}
+
+template <int HD, int W, bool F16, bool FP8>
+__global__ void __launch_bounds__(TreeLayout<HD, W, FP8>::THREADS, 1)
+tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+                         const __grid_constant__ TreeTcArgs p) {
+  using L = TreeLayout<HD, W, FP8>;
+  constexpr bool PV_F16 = F16 && !FP8;          // type of P and V
+  const TreeArgs &a = p.a;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  uint64_t *bars = reinterpret_cast<uint64_t *>(smem + L::BAR);
+  uint64_t *q_full = bars, *q_empty = bars + 1, *o_full = bars + 2, *o_empty = bars + 3, *x_full = bars + 4;
+  uint64_t *s_full = bars + 5, *p_ready = bars + 7;                              // [2] each
+  uint64_t *k_full = bars + 9, *k_empty = k_full + 4, *v_full = k_empty + 4, *v_empty = v_full + 4;      // rings of up to 4
+  uint64_t *c_full = v_empty + 4, *c_empty = c_full + 5;                         // rings of up to 5 (FP8 codes)
+  uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(c_empty + 5);
+  volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
+  volatile int *bad_item = reinterpret_cast<volatile int *>(tmem_slot + 2);      // [2]
+  int *start = reinterpret_cast<int *>(tmem_slot + 4);                           // first sequence, units before the range in it
+  float2 *ml = reinterpret_cast<float2 *>(smem + L::ML);                         // [item & 1][stream][128]
+  float *scales = reinterpret_cast<float *>(smem + L::SC);                       // [tile & 3][K, V][128]
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int group_tokens = W * p.npt, rep = a.n_q / a.n_kv;
+
+  // ---- this CTA's range of units: prefix sums over the sequences (in the ring's memory, not yet in use)
+  int *warp_sum_s = reinterpret_cast<int *>(smem);
+  const int per_thread = (a.n_seqs + L::THREADS - 1) / L::THREADS;
+  const int b_lo = min(a.n_seqs, (int)threadIdx.x * per_thread), b_hi = min(a.n_seqs, b_lo + per_thread);
+  int mine = 0;
+  for (int b = b_lo; b < b_hi; ++b) {
+    if (blockIdx.x == 0) { int x, y, z; tree_lengths(a, b, x, y, z, true); }
+    mine += units_of(a, seq_shape(a, b, group_tokens));
+  }
+  int inc = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int x = __shfl_up_sync(0xffffffffu, inc, o);
+    if (lane >= o) inc += x;
+  }
+  if (lane == 31) warp_sum_s[warp] = inc;
+  __syncthreads();
+  int before = inc - mine, total = 0;
+  for (int w = 0; w < L::WARPS; ++w) {
+    if (w < warp) before += warp_sum_s[w];
+    total += warp_sum_s[w];
+  }
+  const int per = (total + (int)gridDim.x - 1) / (int)gridDim.x;
+  const int u0 = min((long long)total, (long long)blockIdx.x * per), units = min(total - u0, per);
+  if (units <= 0) return;
+  if (u0 >= before && u0 < before + mine) {
+    int at = before;
+    for (int b = b_lo; b < b_hi; ++b) {
+      const int n = units_of(a, seq_shape(a, b, group_tokens));
+      if (u0 < at + n) { start[0] = b; start[1] = u0 - at; break; }
+      at += n;
+    }
+  }
+
+  if (threadIdx.x == 0) {
+    tc::mbar_init(tc::smem_u32(q_full), 1);
+    tc::mbar_init(tc::smem_u32(q_empty), 1);
+    tc::mbar_init(tc::smem_u32(o_full), 1);
+    tc::mbar_init(tc::smem_u32(o_empty), 8);
+    tc::mbar_init(tc::smem_u32(x_full), 8);
+    for (int s = 0; s < 2; ++s) {
+      tc::mbar_init(tc::smem_u32(&s_full[s]), 1);
+      tc::mbar_init(tc::smem_u32(&p_ready[s]), 4);
+    }
+    for (int s = 0; s < 4; ++s) {
+      tc::mbar_init(tc::smem_u32(&k_full[s]), FP8 ? 4 : 1);
+      tc::mbar_init(tc::smem_u32(&k_empty[s]), 1);
+      tc::mbar_init(tc::smem_u32(&v_full[s]), FP8 ? 4 : 1);
+      tc::mbar_init(tc::smem_u32(&v_empty[s]), 1);
+    }
+    for (int s = 0; s < 5; ++s) {
+      tc::mbar_init(tc::smem_u32(&c_full[s]), 1);
+      tc::mbar_init(tc::smem_u32(&c_empty[s]), 4);
+    }
+    *abort_flag = 0;
+    bad_item[0] = bad_item[1] = 0;
+    tc::fence_barrier_init();
+    tc::tma_prefetch_desc(&tmQ);
+    tc::tma_prefetch_desc(&tmK);
+    tc::tma_prefetch_desc(&tmV);
+  }
+  if (warp == 1) tc::tmem_alloc(tc::smem_u32(tmem_slot), 512);
+  tc::tc_fence_before_sync();
+  __syncthreads();
+  tc::tc_fence_after_sync();
+  const uint32_t tmem_base = *tmem_slot;
+  // tensor-memory columns: S0 [0, 128) S1 [128, 256) O0 [256, 256 + HD) O1 [384, 384 + HD); P_w over the first 64 of S_w
+  Pieces it;
+  it.begin(a, start[0], start[1], units, group_tokens);
+  auto wait = [&](uint64_t *bar, uint32_t parity) { return tt_wait(tc::smem_u32(bar), parity, abort_flag, a.status); };
+
+  if (warp == 0) {
+    if (lane == 0) {
+      // ------------------------------------------------------------------ K / V tiles (FP8: their codes, K and V in turn)
+      int kc = 0, vc = 0, cc = 0;
+      bool ok = true;
+      int row = tile_row(a, it.b, it.kt0);
+      do {
+        for (int j = it.kt0; j < it.kt1 && ok; ++j) {
+          const int now = row;
+          if (j + 1 < it.kt1) row = tile_row(a, it.b, j + 1);          // (the table's answer travels while this tile waits)
+          if constexpr (FP8) {
+            for (int kv = 0; kv < 2 && ok; ++kv, ++cc) {
+              const int s = cc % L::CS;
+              ok = wait(&c_empty[s], ((cc / L::CS) & 1) ^ 1);
+              if (!ok) break;
+              const uint32_t bar = tc::smem_u32(&c_full[s]);
+              tc::mbar_expect_tx(bar, L::CODE_TILE);
+              tc::tma_load_2d(tc::smem_u32(smem + L::C + s * L::CODE_TILE), kv ? &tmV : &tmK, bar, it.h * (HD / 2), now);
+            }
+          } else {
+            int s = kc % L::KS;
+            ok = wait(&k_empty[s], ((kc / L::KS) & 1) ^ 1);
+            if (!ok) break;
+            uint32_t bar = tc::smem_u32(&k_full[s]);
+            tc::mbar_expect_tx(bar, L::TILE);
+            for (int c = 0; c < L::CHUNKS; ++c)
+              tc::tma_load_2d(tc::smem_u32(smem + L::K + s * L::TILE + c * L::CHUNK), &tmK, bar, it.h * HD + c * 64, now);
+            ++kc;
+            s = vc % L::VS;
+            ok = wait(&v_empty[s], ((vc / L::VS) & 1) ^ 1);
+            if (!ok) break;
+            bar = tc::smem_u32(&v_full[s]);
+            tc::mbar_expect_tx(bar, L::TILE);
+            for (int c = 0; c < L::CHUNKS; ++c)
+              tc::tma_load_2d(tc::smem_u32(smem + L::V + s * L::TILE + c * L::CHUNK), &tmV, bar, it.h * HD + c * 64, now);
+            ++vc;
+          }
+        }
+        if (!ok || !it.next(a)) break;
+        row = tile_row(a, it.b, it.kt0);
+      } while (true);
+    }
+  } else if (warp == 10) {
+    if (lane == 0) {
+      // ------------------------------------------------------------------ query tiles, as soon as the last piece's Q K^T are done
+      int item = 0;
+      do {
+        if (!wait(q_empty, (item & 1) ^ 1)) break;
+        const uint32_t bar = tc::smem_u32(q_full);
+        tc::mbar_expect_tx(bar, W * L::CHUNKS * p.npt * rep * 128);
+        for (int w = 0; w < W; ++w)
+          for (int c = 0; c < L::CHUNKS; ++c)
+            tc::tma_load_3d(tc::smem_u32(smem + L::Q + w * L::TILE + c * L::CHUNK), &tmQ, bar, c * 64, it.h * rep, it.s.tok0 + (it.g * W + w) * p.npt);
+        ++item;
+      } while (it.next(a));
+    }
+  } else if (warp == 1) {
+    // -------------------------------------------------------------------- MMA issuer (one elected lane)
+    const bool leader = tc::elect_one();
+    constexpr uint32_t idesc_qk = tc::umma_idesc(128, TT_KEYS, 0, 0, F16, F16);
+    constexpr uint32_t idesc_pv = tc::umma_idesc(128, HD, 0, 1, PV_F16, PV_F16);
+    const uint64_t q_desc = tc::umma_desc_sw128(tc::smem_u32(smem + L::Q), 16, 1024);
+    const uint64_t k_desc = tc::umma_desc_sw128(tc::smem_u32(smem + L::K), 16, 1024);
+    const uint64_t v_desc = tc::umma_desc_sw128(tc::smem_u32(smem + L::V), L::CHUNK, 1024);
+    int kc = 0, vc = 0, item = 0, sc0 = 0, sc1 = 0;
+    bool ok = true;
+    do {
+      const int nt = it.kt1 - it.kt0, steps = W == 2 ? 2 * nt : nt;
+      // S of a step; steps alternate between the streams.  The stream's last P V was issued before, and runs before.
+      auto issue_qk = [&](int step) -> bool {
+        const int w = step & 1, s = kc % L::KS;
+        if (W == 1 || w == 0) {
+          if (!wait(&k_full[s], (kc / L::KS) & 1)) return false;
+          tc::tc_fence_after_sync();
+        }
+        if (leader) {
+          const uint64_t qd = q_desc + (uint64_t)((W == 2 ? w : 0) * (L::TILE >> 4)), kd = k_desc + (uint64_t)(s * (L::TILE >> 4));
+#pragma unroll
+          for (int kk = 0; kk < HD / 16; ++kk) {
+            const uint32_t off = ((kk >> 2) * L::CHUNK + (kk & 3) * 32) >> 4;
+            tc::umma_ss(tmem_base + w * 128, qd + off, kd + off, idesc_qk, kk != 0);
+          }
+          tc::umma_commit(tc::smem_u32(&s_full[w]));
+          if (W == 1 || w == 1) tc::umma_commit(tc::smem_u32(&k_empty[s]));
+          if (step == steps - 1) tc::umma_commit(tc::smem_u32(q_empty));
+        }
+        if (W == 1 || w == 1) ++kc;
+        return true;
+      };
+      ok = wait(q_full, item & 1);
+      tc::tc_fence_after_sync();
+      ok = ok && issue_qk(0);
+      for (int step = 0; step < steps && ok; ++step) {
+        if (step + 1 < steps && !(ok = issue_qk(step + 1))) break;
+        const int w = step & 1, s = vc % L::VS;
+        if (W == 1 || w == 0)
+          if (!(ok = wait(&v_full[s], (vc / L::VS) & 1))) break;
+        if (step == 0 && !(ok = wait(o_empty, (item & 1) ^ 1))) break;
+        int &sc = w ? sc1 : sc0;
+        if (!(ok = wait(&p_ready[w], sc & 1))) break;
+        ++sc;
+        tc::tc_fence_after_sync();
+        if (leader) {
+          const uint64_t vd = v_desc + (uint64_t)(s * (L::TILE >> 4));
+#pragma unroll
+          for (int kk = 0; kk < TT_KEYS / 16; ++kk)
+            tc::umma_ts(tmem_base + 256 + w * 128, tmem_base + w * 128 + kk * 8, vd + (uint64_t)((kk * 16 * 128) >> 4), idesc_pv, (step > 1 || kk != 0) ? 1u : 0u);
+          if (W == 1 || w == 1) tc::umma_commit(tc::smem_u32(&v_empty[s]));
+          if (step == steps - 1) tc::umma_commit(tc::smem_u32(o_full));
+        }
+        if (W == 1 || w == 1) ++vc;
+      }
+      ++item;
+      __syncwarp();
+    } while (ok && it.next(a));
+  } else if (warp < 10) {
+    // -------------------------------------------------------------------- softmax: stream w, a query row per thread
+    const int w = (warp - 2) >> 2, quarter = warp & 3, r = quarter * 32 + lane;
+    const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
+    const uint32_t t_s = tmem_base + lane_base + w * 128, t_o = tmem_base + lane_base + 256;
+    const float c = p.scale_log2;
+    int item = 0, sc = 0, tc_count = 0;          // tc_count: tiles of earlier pieces (ring positions)
+    bool ok = true;
+    do {
+      const int nt = it.kt1 - it.kt0;
+      const int node0 = (it.g * W + (W == 2 ? w : 0)) * p.npt;
+      const int rows = min(p.npt, it.s.n - node0) * rep;              // may be <= 0: the pair's second tile
+      const bool warp_active = quarter * 32 < rows, valid = r < rows;
+      const int node = valid ? node0 + r / rep : 0, tok = it.s.tok0 + node;
+      float m_ref = -INFINITY, l = 0.f;
+      bool first = true;
+      for (int j = W == 2 ? 0 : w; j < nt; j += W == 2 ? 1 : 2) {
+        const int tile = tc_count + j;
+        const int j0 = (it.kt0 + j) * TT_KEYS - it.s.past;            // the tile's first key, counted from the first new token
+        const bool edge = j0 > -TT_KEYS;                              // holds new tokens (and perhaps rows behind them)
+        if constexpr (!FP8) {
+          if (edge && (W == 1 || w == 0)) {
+            // V rows that must not meet a zero probability as NaN or infinity (comment at the top)
+            const int s = tile % L::VS, key = j0 + r;
+            if (!(ok = wait(&v_full[s], (tile / L::VS) & 1))) break;
+            if (key >= 0) {
+              uint8_t *vrow = smem + L::V + s * L::TILE + r * 128;
+              bool clear = key >= it.s.n;
+              if (!clear) {
+                uint32_t worst = 0;
+#pragma unroll 1
+                for (int i = 0; i < L::CHUNKS * 8; ++i) {
+                  const uint4 x = *reinterpret_cast<const uint4 *>(vrow + (i >> 3) * L::CHUNK + (i & 7) * 16);
+                  const uint32_t e = F16 ? 0x7c007c00u : 0x7f807f80u, xs[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                  for (int q4 = 0; q4 < 4; ++q4) worst |= ((xs[q4] & e & 0xffff0000u) == (e & 0xffff0000u)) | ((xs[q4] & e & 0xffffu) == (e & 0xffffu));
+                }
+                if (worst) { clear = true; bad_item[item & 1] = item + 1; }
+              }
+              if (clear) {
+#pragma unroll 1
+                for (int i = 0; i < L::CHUNKS * 8; ++i)
+                  *reinterpret_cast<uint4 *>(vrow + (i >> 3) * L::CHUNK + (i & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+                tc::fence_proxy_async_smem();
+              }
+            }
+          }
+        }
+        if (!(ok = wait(&s_full[w], sc & 1))) break;
+        tc::tc_fence_after_sync();
+        ++sc;
+        const float *ksc = nullptr, *vsc = nullptr;
+        if constexpr (FP8) {
+          // (the widening warps wrote both scales of the tile's rows before they announced its V rows)
+          ksc = scales + (tile & 3) * 256;
+          vsc = ksc + 128;
+          if (!(ok = wait(&v_full[tile % L::VS], (tile / L::VS) & 1))) break;
+        }
+        if (warp_active) {
+          uint32_t words[4] = {0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu};
+          if (edge) {
+#pragma unroll
+            for (int q4 = 0; q4 < 4; ++q4) words[q4] = valid ? sees_word(a, tok, node, it.s.n, j0 + 32 * q4) : 0u;
+          }
+          // scores in 64-column halves; kept in registers between the maximum and the exponentials, except with an FP8 cache, whose
+          // four more warps leave no room: there they are read twice
+          constexpr int KEEP = FP8 ? 64 : 128;
+          uint32_t s[KEEP];
+          auto load_half = [&](int hf, uint32_t *d) {
+            tc::tmem_ld_32x32b_x32p(t_s + hf * 64, d);
+            tc::tmem_ld_32x32b_x32p(t_s + hf * 64 + 32, d + 32);
+            tc::tmem_ld_wait();
+            if constexpr (FP8) {
+#pragma unroll
+              for (int i = 0; i < 64; i += 4) {
+                const float4 k4 = *reinterpret_cast<const float4 *>(ksc + hf * 64 + i);
+                d[i] = __float_as_uint(__uint_as_float(d[i]) * k4.x);
+                d[i + 1] = __float_as_uint(__uint_as_float(d[i + 1]) * k4.y);
+                d[i + 2] = __float_as_uint(__uint_as_float(d[i + 2]) * k4.z);
+                d[i + 3] = __float_as_uint(__uint_as_float(d[i + 3]) * k4.w);
+              }
+            }
+            if (edge) {
+#pragma unroll
+              for (int i = 0; i < 64; ++i)
+                if (!((words[hf * 2 + (i >> 5)] >> (i & 31)) & 1u)) d[i] = 0xff800000u;      // -inf
+            }
+          };
+          float m0 = -INFINITY, m1 = -INFINITY, m2 = -INFINITY, m3 = -INFINITY;
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf) {
+            uint32_t *d = s + (FP8 ? 0 : hf * 64);
+            load_half(hf, d);
+#pragma unroll
+            for (int i = 0; i < 64; i += 8) {
+              m0 = tc::max3(m0, __uint_as_float(d[i]), __uint_as_float(d[i + 1]));
+              m1 = tc::max3(m1, __uint_as_float(d[i + 2]), __uint_as_float(d[i + 3]));
+              m2 = tc::max3(m2, __uint_as_float(d[i + 4]), __uint_as_float(d[i + 5]));
+              m3 = tc::max3(m3, __uint_as_float(d[i + 6]), __uint_as_float(d[i + 7]));
+            }
+          }
+          const float mx = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3));
+          const bool need = first || (mx - m_ref) * c > TT_RESCALE;
+          const float m_new = need ? mx : m_ref;
+          if (!first && __any_sync(0xffffffffu, need && valid)) {
+            // S of this step is complete, so every earlier P V of the stream has retired: O may be rescaled
+            const float f = need ? tt_exp2((m_ref - m_new) * c) : 1.f;
+            l *= f;
+#pragma unroll 1
+            for (int ch = 0; ch < HD / 16; ++ch) {
+              uint32_t o[16];
+              tc::tmem_ld_32x32b_x16(t_o + w * 128 + ch * 16, o);
+              tc::tmem_ld_wait();
+#pragma unroll
+              for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+              tc::tmem_st_32x32b_x16(t_o + w * 128 + ch * 16, o);
+            }
+          }
+          m_ref = m_new;
+          const float neg_mc = m_ref == -INFINITY ? 0.f : -m_ref * c;       // (a row that sees nothing yet: every exponential is 0)
+          float l0 = 0.f, l1 = 0.f, l2 = 0.f, l3 = 0.f;
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf) {
+            uint32_t *d = s + (FP8 ? 0 : hf * 64);
+            if constexpr (FP8) load_half(hf, d);
+            uint32_t packed[32];
+#pragma unroll
+            for (int i = 0; i < 64; i += 4) {
+              float p0 = tt_exp2(fmaf(__uint_as_float(d[i]), c, neg_mc)), p1 = tt_exp2(fmaf(__uint_as_float(d[i + 1]), c, neg_mc));
+              float p2 = tt_exp2(fmaf(__uint_as_float(d[i + 2]), c, neg_mc)), p3 = tt_exp2(fmaf(__uint_as_float(d[i + 3]), c, neg_mc));
+              l0 += p0; l1 += p1; l2 += p2; l3 += p3;
+              if constexpr (FP8) {
+                const float4 v4 = *reinterpret_cast<const float4 *>(vsc + hf * 64 + i);
+                p0 *= v4.x; p1 *= v4.y; p2 *= v4.z; p3 *= v4.w;
+                if (edge) {                                                  // (the scale of an unseen row may be anything)
+                  const uint32_t wd = words[hf * 2 + (i >> 5)] >> (i & 31);
+                  p0 = (wd & 1u) ? p0 : 0.f; p1 = (wd & 2u) ? p1 : 0.f; p2 = (wd & 4u) ? p2 : 0.f; p3 = (wd & 8u) ? p3 : 0.f;
+                }
+              }
+              packed[i / 2] = PV_F16 ? tc::pack_f16x2(p0, p1) : tc::pack_bf16x2(p0, p1);
+              packed[i / 2 + 1] = PV_F16 ? tc::pack_f16x2(p2, p3) : tc::pack_bf16x2(p2, p3);
+            }
+            tc::tmem_st_32x32b_x32(t_s + hf * 32, packed);      // over scores that have been read for the last time
+          }
+          l += (l0 + l1) + (l2 + l3);
+          first = false;
+          tc::tmem_st_wait();
+        }
+        tc::tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(tc::smem_u32(&p_ready[w]));
+      }
+      if (!ok) break;
+      // ---- the piece's result.  Both streams meet here once (W = 1: to join their halves of the keys).
+      ml[((item & 1) * 2 + w) * 128 + r] = make_float2(m_ref, l);
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(tc::smem_u32(x_full));
+      if (!(ok = wait(x_full, item & 1)) || !(ok = wait(o_full, item & 1))) break;
+      tc::tc_fence_after_sync();
+      if (warp_active) {
+        float m = m_ref, f0 = 1.f, f1 = 0.f;
+        if constexpr (W == 1) {
+          const float2 x0 = ml[((item & 1) * 2) * 128 + r], x1 = ml[((item & 1) * 2 + 1) * 128 + r];
+          m = fmaxf(x0.x, x1.x);
+          f0 = x0.x == -INFINITY ? 0.f : tt_exp2((x0.x - m) * c);
+          f1 = x1.x == -INFINITY ? 0.f : tt_exp2((x1.x - m) * c);
+          l = x0.y * f0 + (nt > 1 ? x1.y * f1 : 0.f);
+        }
+        const bool whole = it.whole(), bad = bad_item[item & 1] == item + 1;
+        const float inv = whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
+        const size_t head = (size_t)tok * a.n_q + it.h * rep + (valid ? r % rep : 0);
+        const int slot = (int)blockIdx.x * 2 + (it.kt0 == 0 ? 1 : 0);
+        const int srow = (W == 2 ? w : 0) * p.npt * rep + r;
+        float *part = a.scratch + ((size_t)slot * p.slot_rows + srow) * (HD + 2);
+        constexpr int COLS = W == 1 ? HD / 2 : HD;
+        const int col0 = W == 1 ? w * COLS : 0;
+        if (valid && col0 == 0 && (W == 2 || w == 0)) {
+          if (!whole) *reinterpret_cast<float2 *>(part) = make_float2(m * c, l);
+          else if (a.lse) a.lse[head] = l == 0.f ? -INFINITY : m * a.scale + logf(l);
+        }
+#pragma unroll 1
+        for (int ch = 0; ch < COLS / 32; ++ch) {
+          const int d0 = col0 + ch * 32;
+          uint32_t x[32];
+          float o[32];
+          tc::tmem_ld_32x32b_x32(t_o + (W == 2 ? w * 128 : 0) + d0, x);
+          tc::tmem_ld_wait();
+#pragma unroll
+          for (int i = 0; i < 32; ++i) o[i] = W == 1 ? __uint_as_float(x[i]) * f0 : __uint_as_float(x[i]);
+          if (W == 1 && nt > 1) {
+            tc::tmem_ld_32x32b_x32(t_o + 128 + d0, x);
+            tc::tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 32; ++i) o[i] = fmaf(__uint_as_float(x[i]), f1, o[i]);
+          }
+          if (valid) {
+            if (bad) {
+              // drafted tokens of this piece whose V row was not finite: what the rows that see them get from it
+#pragma unroll 1
+              for (int q2 = max(0, it.kt0 * TT_KEYS - it.s.past); q2 < min(it.s.n, it.kt1 * TT_KEYS - it.s.past); ++q2) {
+                const int row = tree_row(a, it.b, it.s.past + q2);
+                if (row < 0 || !tree_sees(a, tok, node, it.s.past, it.s.n, it.s.past + q2)) continue;
+                const uint16_t *v = reinterpret_cast<const uint16_t *>(a.v) + ((size_t)row * a.n_kv + it.h) * HD + d0;
+                const uint16_t e = F16 ? 0x7c00 : 0x7f80;
+#pragma unroll
+                for (int i = 0; i < 32; ++i) {
+                  const uint16_t bits = v[i];
+                  if ((bits & e) == e) o[i] += F16 ? __half2float(__ushort_as_half(bits)) : __uint_as_float((uint32_t)bits << 16);
+                }
+              }
+            }
+            if (whole) {
+              uint32_t y[16];
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                const float e0 = l == 0.f ? 0.f : o[2 * i] * inv, e1 = l == 0.f ? 0.f : o[2 * i + 1] * inv;
+                if constexpr (F16) {
+                  const __half2 h2 = __floats2half2_rn(e0, e1);
+                  y[i] = *reinterpret_cast<const uint32_t *>(&h2);
+                } else {
+                  y[i] = tc::pack_bf16x2(e0, e1);
+                }
+              }
+              uint16_t *dst = reinterpret_cast<uint16_t *>(a.out) + head * HD + d0;
+              if (p.store32) {
+                tc::st_global_v8(dst, y);
+                tc::st_global_v8(dst + 16, y + 8);
+              } else {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) dst[i] = (uint16_t)(y[i >> 1] >> ((i & 1) * 16));
+              }
+            } else {
+              float2 *dst = reinterpret_cast<float2 *>(part + 2 + d0);
+#pragma unroll
+              for (int i = 0; i < 16; ++i) dst[i] = make_float2(o[2 * i], o[2 * i + 1]);
+            }
+          }
+        }
+      }
+      tc::tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(tc::smem_u32(o_empty));
+      tc_count += nt;
+      ++item;
+    } while (it.next(a));
+  } else if constexpr (FP8) {
+    // -------------------------------------------------------------------- widening warps: codes -> swizzled 16-bit tiles, scales
+    const int t = threadIdx.x - 11 * 32;
+    int cc = 0, tile = 0;
+    bool ok = true;
+    do {
+      // a row's scales hang on its page number: the number is asked for two tiles ahead, the scales one
+      auto row_of = [&](int j) {
+        const int key = j * TT_KEYS + t;
+        return j < it.kt1 && key < it.s.past + it.s.n ? tree_row(a, it.b, key) : -1;
+      };
+      int row1 = row_of(it.kt0), row2 = row_of(it.kt0 + 1);
+      float sk1 = row1 >= 0 ? a.k_scale[row1] : 0.f, sv1 = row1 >= 0 ? a.v_scale[row1] : 0.f;
+      for (int j = it.kt0; j < it.kt1 && ok; ++j, ++tile) {
+        const float sk = sk1, sv = sv1;
+        sk1 = row2 >= 0 ? a.k_scale[row2] : 0.f;
+        sv1 = row2 >= 0 ? a.v_scale[row2] : 0.f;
+        row2 = row_of(j + 2);
+        for (int kv = 0; kv < 2 && ok; ++kv, ++cc) {
+          const int cs = cc % L::CS, ds = kv ? tile % L::VS : 0;
+          const uint8_t *src = smem + L::C + cs * L::CODE_TILE;
+          uint8_t *dst = smem + (kv ? L::V : L::K) + ds * L::TILE;
+          ok = wait(&c_full[cs], (cc / L::CS) & 1) && (kv ? wait(&v_empty[ds], ((tile / L::VS) & 1) ^ 1) : wait(&k_empty[0], (tile & 1) ^ 1));
+          if (!ok) break;
+          scales[(tile & 3) * 256 + kv * 128 + t] = kv ? sv : sk;
+#pragma unroll 4
+          for (int i = t; i < L::CODE_TILE / 16; i += 128) {
+            const int at = i * 16;
+            const uint4 x = *reinterpret_cast<const uint4 *>(src + at);
+            const int rr = at / HD, col = at % HD;
+            uint4 y0, y1;
+            const bool half = kv ? PV_F16 : F16;
+            widen4(x.x, y0.x, y0.y, half);
+            widen4(x.y, y0.z, y0.w, half);
+            widen4(x.z, y1.x, y1.y, half);
+            widen4(x.w, y1.z, y1.w, half);
+            uint8_t *line = dst + (col >> 6) * L::CHUNK + rr * 128;
+            const int u = (col & 63) >> 3;
+            *reinterpret_cast<uint4 *>(line + (((u) ^ (rr & 7)) << 4)) = y0;
+            *reinterpret_cast<uint4 *>(line + (((u + 1) ^ (rr & 7)) << 4)) = y1;
+          }
+          tc::fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) {
+            tc::mbar_arrive(tc::smem_u32(&c_empty[cs]));
+            tc::mbar_arrive(tc::smem_u32(kv ? &v_full[ds] : &k_full[0]));
+          }
+        }
+      }
+    } while (ok && it.next(a));
+  }
+  tc::tc_fence_before_sync();
+  __syncthreads();
+  if (warp == 1) {
+    __syncwarp();
+    tc::tc_fence_after_sync();
+    tc::tmem_dealloc(tmem_base, 512);
+  }
+}
+
+// joins the partial results of the pieces that a (sequence, group, head) was cut into: block per new token
+constexpr int TJ_THREADS = 256;
+template <int HD, bool F16>
+__global__ void __launch_bounds__(TJ_THREADS) tree_attention_tc_join_kernel(TreeTcArgs p, int ctas, int tiles_per_group) {
+  const TreeArgs &a = p.a;
+  const int t = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int group_tokens = tiles_per_group * p.npt, rep = a.n_q / a.n_kv;
+  __shared__ int s_total[TJ_THREADS / 32], s_before[TJ_THREADS / 32], s_b;
+  if (tid == 0) s_b = -1;
+  __syncthreads();
+  int total = 0, before = 0;
+  for (int b = tid; b < a.n_seqs; b += TJ_THREADS) {
+    const SeqShape s = seq_shape(a, b, group_tokens);
+    const int u = units_of(a, s);
+    total += u;
+    if (s.tok0 + s.n <= t) before += u;
+    else if (s.tok0 <= t) s_b = b;
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    total += __shfl_xor_sync(0xffffffffu, total, o);
+    before += __shfl_xor_sync(0xffffffffu, before, o);
+  }
+  if (lane == 0) { s_total[warp] = total; s_before[warp] = before; }
+  __syncthreads();
+  const int b = s_b;
+  if (b < 0) return;                                   // a row behind the last sequence
+  total = before = 0;
+#pragma unroll
+  for (int w = 0; w < TJ_THREADS / 32; ++w) { total += s_total[w]; before += s_before[w]; }
+  const SeqShape s = seq_shape(a, b, group_tokens);
+  const int per = (total + ctas - 1) / ctas;
+  const int node = t - s.tok0, g = node / group_tokens, srow0 = (node - g * group_tokens) * rep;
+  constexpr int LANES = HD / 4, PER_PASS = TJ_THREADS / LANES;
+  const int d = (tid % LANES) * 4;
+  for (int hq = tid / LANES; hq < a.n_q; hq += PER_PASS) {
+    const int h = hq / rep;
+    const int first = before + (g * a.n_kv + h) * s.tiles, last = first + s.tiles - 1;
+    const int c0 = first / per, c1 = last / per;
+    if (c0 == c1) continue;                            // whole: already in `out`
+    const int srow = srow0 + hq % rep;
+    // the first piece starts at the item's first tile: its CTA's slot 1; the others are the first piece of theirs: slot 0
+    auto piece = [&](int ct) { return a.scratch + ((size_t)(ct * 2 + (ct == c0 ? 1 : 0)) * p.slot_rows + srow) * (HD + 2); };
+    float m = -INFINITY;
+#pragma unroll 4
+    for (int ct = c0; ct <= c1; ++ct) m = fmaxf(m, piece(ct)[0]);
+    float l = 0.f, o0 = 0.f, o1 = 0.f, o2 = 0.f, o3 = 0.f;
+#pragma unroll 4
+    for (int ct = c0; ct <= c1; ++ct) {
+      const float *x = piece(ct);
+      const float2 ml = *reinterpret_cast<const float2 *>(x), u = *reinterpret_cast<const float2 *>(x + 2 + d), v = *reinterpret_cast<const float2 *>(x + 4 + d);
+      const float f = ml.x == -INFINITY ? 0.f : tt_exp2(ml.x - m);
+      if (f == 0.f && ml.y == 0.f) continue;           // saw nothing
+      l = fmaf(ml.y, f, l);
+      o0 = fmaf(u.x, f, o0); o1 = fmaf(u.y, f, o1); o2 = fmaf(v.x, f, o2); o3 = fmaf(v.y, f, o3);
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    if (l == 0.f) o0 = o1 = o2 = o3 = 0.f;
+    const size_t head = (size_t)t * a.n_q + hq;
+    uint16_t y[4];
+    if constexpr (F16) {
+      y[0] = __half_as_ushort(__float2half_rn(o0 * inv)); y[1] = __half_as_ushort(__float2half_rn(o1 * inv));
+      y[2] = __half_as_ushort(__float2half_rn(o2 * inv)); y[3] = __half_as_ushort(__float2half_rn(o3 * inv));
+    } else {
+      y[0] = __bfloat16_as_ushort(__float2bfloat16_rn(o0 * inv)); y[1] = __bfloat16_as_ushort(__float2bfloat16_rn(o1 * inv));
+      y[2] = __bfloat16_as_ushort(__float2bfloat16_rn(o2 * inv)); y[3] = __bfloat16_as_ushort(__float2bfloat16_rn(o3 * inv));
+    }
+    uint16_t *dst = reinterpret_cast<uint16_t *>(a.out) + head * HD + d;
+    if (p.store32) *reinterpret_cast<uint2 *>(dst) = make_uint2((uint32_t)y[0] | (uint32_t)y[1] << 16, (uint32_t)y[2] | (uint32_t)y[3] << 16);
+    else { dst[0] = y[0]; dst[1] = y[1]; dst[2] = y[2]; dst[3] = y[3]; }
+    if (a.lse && d == 0) a.lse[head] = l == 0.f ? -INFINITY : m * 0.6931471805599453f + logf(l);
+  }
+}
+
+// rows of a partial result: those of a group of query tiles, or all that a call has for one KV head
+int tc_slot_rows(int total_new, int n_q, int n_kv) {
+  const long long all = (long long)total_new * (n_q / n_kv);
+  return all < 256 ? (int)all : 256;
+}
+size_t tc_scratch(int total_new, int n_q, int hd) {
+  // (independent of the group size: a call's rows of one KV head are at most all its rows)
+  return (size_t)num_sms() * 2 * tc_slot_rows(total_new, n_q, 1) * (hd + 2) * sizeof(float);
+}
+
+// shapes and addresses that the tensor-core form takes (TMA: 16-byte boundaries and strides)
+bool tc_supported(const TreeArgs &a, bool q16, bool fp8) {
+  if (!q16 || (a.hd != 64 && a.hd != 128) || a.n_q / a.n_kv > 128) return false;
+  const uintptr_t at = (uintptr_t)a.q | (uintptr_t)a.k | (uintptr_t)a.v | (uintptr_t)(a.q_stride * 2);
+  return (at & 15) == 0 && a.cache_rows < (1 << 30) && (!fp8 || (a.n_kv * a.hd) % 16 == 0);
+}
+
+template <int HD, int W, bool F16, bool FP8>
+int32_t launch_tc(const TreeTcArgs &p, int max_kv, cudaStream_t st) {
+  using L = TreeLayout<HD, W, FP8>;
+  static_assert(L::BYTES <= 232448, "shared memory of one CTA");
+  const TreeArgs &a = p.a;
+  const int rep = a.n_q / a.n_kv;
+  CUtensorMap tq, tk, tv;
+  const uint64_t cols = (uint64_t)a.n_kv * HD / (FP8 ? 2 : 1);             // codes travel as pairs of bytes
+  if (make_tmap_3d_bf16(&tq, a.q, HD, a.n_q, a.total_new, HD, a.q_stride, 64, rep, p.npt) ||
+      make_tmap_2d_bf16(&tk, a.k, a.cache_rows, cols, cols, TT_KEYS, FP8 ? HD / 2 : 64, !FP8) ||
+      make_tmap_2d_bf16(&tv, a.v, a.cache_rows, cols, cols, TT_KEYS, FP8 ? HD / 2 : 64, !FP8))
+    return report_error(SWIFTKV_ERR_CUDA, "tensor map");
+  auto kernel = tree_attention_tc_kernel<HD, W, F16, FP8>;
+  if (ensure_dynamic_smem(reinterpret_cast<const void *>(kernel), L::BYTES)) return report_error(SWIFTKV_ERR_CUDA, "shared memory");
+  const long long groups = (a.max_new + W * p.npt - 1) / (W * p.npt), tiles = ((long long)max_kv + TT_KEYS - 1) / TT_KEYS;
+  const long long most = groups * tiles * a.n_kv * a.n_seqs;
+  if (most > 0x7fffffffLL) return report_error(SWIFTKV_ERR_UNSUPPORTED, "too many key tiles for one launch");
+  const int grid = (int)(most < num_sms() ? most : num_sms());
+  kernel<<<grid, L::THREADS, L::BYTES, st>>>(tq, tk, tv, p);
+  cudaError_t e = cudaGetLastError();
+  if (e == cudaSuccess && grid > 1) {
+    tree_attention_tc_join_kernel<HD, F16><<<a.total_new, TJ_THREADS, 0, st>>>(p, grid, W);
+    e = cudaGetLastError();
+  }
+  return e == cudaSuccess ? SWIFTKV_OK : report_error(SWIFTKV_ERR_CUDA, cudaGetErrorString(e));
+}
+
+template <int HD, bool F16>
+int32_t launch_tc_for(const TreeArgs &a, bool fp8, int max_kv, cudaStream_t st) {
+  TreeTcArgs p{};
+  p.a = a;
+  const int rep = a.n_q / a.n_kv;
+  p.npt = 128 / rep;
+  p.slot_rows = tc_slot_rows(a.total_new, a.n_q, a.n_kv);
+  p.scale_log2 = a.scale * 1.4426950408889634f;
+  p.store32 = ((uintptr_t)a.out & 31) == 0;
+  if (fp8) return launch_tc<HD, 1, F16, true>(p, max_kv, st);
+  // more rows than one query tile holds: two tiles share the key tiles of a pass
+  return a.max_new > p.npt ? launch_tc<HD, 2, F16, false>(p, max_kv, st) : launch_tc<HD, 1, F16, false>(p, max_kv, st);
+}
+
 }  // namespace
 }  // namespace skv
 
@@ -228,7 +1030,10 @@ using namespace skv;
 
 extern "C" size_t swiftkv_tree_attention_scratch_bytes(int32_t total_new, int32_t max_kv, int32_t n_q_heads, int32_t head_dim) {
   if (total_new < 1 || max_kv < 1 || n_q_heads < 1 || head_dim < 1 || head_dim > 256) return 0;
-  return simt_scratch(total_new, max_kv, n_q_heads, head_dim);
+  const size_t simt = simt_scratch(total_new, max_kv, n_q_heads, head_dim);
+  if (head_dim != 64 && head_dim != 128) return simt;
+  const size_t tcs = tc_scratch(total_new, n_q_heads, head_dim);
+  return simt > tcs ? simt : tcs;
 }
 
 extern "C" int32_t swiftkv_tree_attention(const void *q, int64_t q_stride, int32_t q_dtype, const void *k_cache, const void *v_cache,
@@ -264,6 +1069,10 @@ extern "C" int32_t swiftkv_tree_attention(const void *q, int64_t q_stride, int32
   a.scale = softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)head_dim);
   a.status = status;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
+  if (tc_supported(a, q_dtype != SWIFTKV_DTYPE_F32, fp8)) {
+    if (q_dtype == SWIFTKV_DTYPE_BF16) return head_dim == 64 ? launch_tc_for<64, false>(a, fp8, max_kv, st) : launch_tc_for<128, false>(a, fp8, max_kv, st);
+    return head_dim == 64 ? launch_tc_for<64, true>(a, fp8, max_kv, st) : launch_tc_for<128, true>(a, fp8, max_kv, st);
+  }
   if (fp8) {
     if (q_dtype == SWIFTKV_DTYPE_F32) return launch_simt<float, fp8e4>(a, max_kv, st);
     if (q_dtype == SWIFTKV_DTYPE_BF16) return launch_simt<bf16, fp8e4>(a, max_kv, st);
