@@ -567,7 +567,7 @@ int32_t swiftkv_qk_norm_rope_bwd(const void *dq, const void *dk, const void *q, 
  *   out         : [total_new][n_q_heads][head_dim] in q_dtype; lse (nullable): fp32 [total_new][n_q_heads], natural logarithm of the
  *                 softmax's denominator.  Rows of tokens that belong to no sequence are left as they were
  *   softmax_scale : 0 means 1/sqrt(head_dim)
- *   scratch     : >= swiftkv_tree_attention_scratch_bytes(...) bytes (may be null where that is 0), 16-byte aligned, not shared with
+ *   scratch     : >= swiftkv_tree_attention_scratch_bytes(...) bytes (may be null where that is 0), 256-byte aligned, not shared with
  *                 a call that may run at the same time; sufficient for any smaller total_new and max_kv too
  * head_dim <= 256.  Errors: INVALID_ARG, WORKSPACE_SMALL, UNSUPPORTED, CUDA. */
 size_t  swiftkv_tree_attention_scratch_bytes(int32_t total_new, int32_t max_kv, int32_t n_q_heads, int32_t head_dim);

@@ -396,6 +396,7 @@ __global__ void __launch_bounds__(LP_THREADS + 32, 2) token_logprobs_kernel(LpAr
   if (warp == LP_WARPS) {
     // ---- the warp that joins rows up
     int turn = 0;
+    bool alive = true;
     for (int row = row0; row < a.rows; row += row_step, ++turn) {
       const int par = turn & 1;
       const T *x = reinterpret_cast<const T *>(a.logits) + (size_t)row * a.stride;
@@ -404,10 +405,10 @@ __global__ void __launch_bounds__(LP_THREADS + 32, 2) token_logprobs_kernel(LpAr
       const float tgt_v = tgt >= 0 && tgt < a.vocab ? lp_load(x + tgt) : 0.f;
       const uint32_t done = tc::smem_u32(&sh.row_done[par]);
       const long long t0 = clock64();
-      while (!tc::mbar_try_wait(done, (turn >> 1) & 1)) {
+      while (alive && !tc::mbar_try_wait(done, (turn >> 1) & 1)) {
         if (clock64() - t0 > tc::WAIT_LIMIT_CLOCKS) {
           if (lane == 0) atomicOr(a.status, STATUS_TIMEOUT);
-          break;
+          alive = false;
         }
         if (TOP) {
           const uint32_t bound = lp_bound(sh, par, k);
@@ -439,6 +440,13 @@ __global__ void __launch_bounds__(LP_THREADS + 32, 2) token_logprobs_kernel(LpAr
     }
     return;
   }
+  bool alive = true;            // a wait that ran out (never, unless something is broken): no further waits or copies
+  auto wait = [&](uint64_t *bar, uint32_t parity) {
+    if (alive && !tc::mbar_wait(tc::smem_u32(bar), parity)) {
+      alive = false;
+      atomicOr(a.status, STATUS_TIMEOUT);
+    }
+  };
   // thread 0 keeps the ring full: chunk p_count of this block's rows, one after the other
   int p_row = row0, p_v = 0, p_end = 0, p_count = 0;
   const uint4 *p_src = nullptr;
@@ -453,10 +461,11 @@ __global__ void __launch_bounds__(LP_THREADS + 32, 2) token_logprobs_kernel(LpAr
     }
   };
   auto fetch = [&]() {          // the next chunk, if there is one; its stage must have been emptied
-    if (p_row >= a.rows) return;
+    if (p_row >= a.rows || !alive) return;
     const int st = p_count % LP_STAGES;
     const uint32_t bar = tc::smem_u32(&sh.full[st]);
-    if (p_count >= LP_STAGES && !tc::mbar_wait(tc::smem_u32(&sh.empty[st]), (p_count / LP_STAGES - 1) & 1)) atomicOr(a.status, STATUS_TIMEOUT);
+    if (p_count >= LP_STAGES) wait(&sh.empty[st], (p_count / LP_STAGES - 1) & 1);
+    if (!alive) return;
     const uint32_t bytes = (uint32_t)min(LP_CHUNK, p_end - p_v) * 16;
     tc::mbar_expect_tx(bar, bytes);
     bulk_load(tc::smem_u32(lp_ring) + st * LP_CHUNK * 16, p_src + p_v, bytes, bar);
@@ -471,7 +480,7 @@ __global__ void __launch_bounds__(LP_THREADS + 32, 2) token_logprobs_kernel(LpAr
   int count = 0, turn = 0;      // chunks and rows consumed
   for (int row = row0; row < a.rows; row += row_step, ++turn) {
     const int par = turn & 1;
-    if (turn > 1 && !tc::mbar_wait(tc::smem_u32(&sh.row_free[par]), ((turn >> 1) - 1) & 1) && lane == 0) atomicOr(a.status, STATUS_TIMEOUT);
+    if (turn > 1) wait(&sh.row_free[par], ((turn >> 1) - 1) & 1);
     const T *x = reinterpret_cast<const T *>(a.logits) + (size_t)row * a.stride;
     const LpRow rw = lp_row<T>(a, row, part);
     const uint4 *xv = reinterpret_cast<const uint4 *>(x + rw.head);
@@ -509,7 +518,7 @@ __global__ void __launch_bounds__(LP_THREADS + 32, 2) token_logprobs_kernel(LpAr
     for (int v0 = rw.v_begin; v0 < rw.v_end; v0 += LP_CHUNK, ++count) {
       const int st = count % LP_STAGES;
       if (tid == 0) fetch();
-      if (!tc::mbar_wait(tc::smem_u32(&sh.full[st]), (count / LP_STAGES) & 1) && lane == 0) atomicOr(a.status, STATUS_TIMEOUT);
+      wait(&sh.full[st], (count / LP_STAGES) & 1);
       const uint4 *chunk = reinterpret_cast<const uint4 *>(lp_ring) + st * LP_CHUNK + tid;
       uint4 raw[LP_UNROLL];
 #pragma unroll

@@ -235,10 +235,14 @@ size_t simt_scratch(int total_new, int max_kv, int n_q, int hd) {
 // Work split: the (sequence, tile group, KV head, key tile) units of a call, in this order, are cut into equal contiguous
 // ranges, one per CTA (one CTA per SM).  The lengths live on the device, so every CTA sums them up for itself.  A range that
 // starts or ends inside a (sequence, group, head) leaves an unnormalised partial result in `scratch` (at most two per CTA),
-// and a second kernel joins those in the order of the keys: deterministic, and balanced for any mix of lengths.
+// and a second kernel joins those in the order of the keys: deterministic, and balanced for any mix of lengths.  Where the
+// longest sequence has two groups, the CTAs form two classes, one per group, that walk over the same keys in step, so that
+// the second one finds them in L2 (a sequence with one group gives each class half of its keys).
 //
-// FP8 rows: TMA brings the codes, four warps widen them to the 16-bit type exactly (every e4m3 number is one) and the fp32
-// scales of the rows enter after Q K^T (K) and into P before its rounding (V).
+// FP8 rows: TMA brings the codes and four warps widen them to IEEE half, exactly (every e4m3 number is one).  Queries in bf16
+// become halves too, each row times a power of two that brings its maximum to 2^14 .. 2^15: what that loses (elements below 2^-38 of the
+// maximum) is below the accumulation's own rounding.  K scales multiply the scores; V scales enter P, whose reference
+// exponent follows the largest scale-weighted probability of the row, so that P keeps the full half precision.
 //
 // What is not seen must not matter: keys behind the sequence and unseen drafts get S = -inf, and the V rows of the last
 // tiles are cleaned in shared memory first (0 * NaN is NaN): rows behind the sequence become zeros, and a drafted token's V row that
@@ -253,7 +257,7 @@ struct TreeLayout {
   static constexpr int CODE_TILE = 128 * HD;
   static constexpr int KS = FP8 ? 1 : (HD == 64 ? 4 : 2), VS = FP8 ? 2 : (HD == 64 ? 4 : (W == 2 ? 2 : 3)), CS = FP8 ? 5 : 0;
   static constexpr int Q = 0, K = W * TILE, V = K + KS * TILE, C = V + VS * TILE, SC = C + CS * CODE_TILE;
-  static constexpr int ML = SC + (FP8 ? 4 * 2 * 128 * 4 : 0);       // scales: 4 tiles x (K, V) x 128
+  static constexpr int ML = SC + (FP8 ? (4 * 3 + 2) * 128 * 4 : 0); // scales: 4 tiles x (K, V, log2 V) x 128; query rows' powers of two x 2
   static constexpr int BAR = ML + 2 * 2 * 128 * 8;                  // (m, l) of both streams, two items
   static constexpr int BYTES = BAR + 512 + 1024;
   static constexpr int WARPS = 11 + (FP8 ? 4 : 0);
@@ -264,6 +268,8 @@ struct TreeTcArgs {
   TreeArgs a;
   int npt;               // new tokens per query tile
   int slot_rows;         // rows of a partial result in scratch
+  int classes;           // 1 or 2 classes of CTAs
+  float *part_o;         // [slot][slot_rows][HD] unnormalised outputs; (m, l) pairs [slot][slot_rows] at a.scratch
   float scale_log2;
   int store32;
 };
@@ -289,47 +295,59 @@ __device__ __forceinline__ float tt_exp2(float x) {
   return y;
 }
 
-// units of a sequence: key tiles x KV heads x groups of W query tiles
-struct SeqShape { int tok0, n, past, tiles, groups; };
-__device__ __forceinline__ SeqShape seq_shape(const TreeArgs &a, int b, int group_tokens) {
+// What a class of CTAs does of a sequence: key tiles [lo, hi) x KV heads x `groups` groups of W query tiles from group g0 on
+struct SeqShape { int tok0, n, past, tiles, lo, hi, g0, groups; };
+struct Split { int group_tokens, classes, cls; };
+__device__ __forceinline__ SeqShape seq_shape(const TreeArgs &a, int b, const Split &sp) {
   SeqShape s;
   tree_lengths(a, b, s.tok0, s.n, s.past, false);
   s.tiles = (s.past + s.n + TT_KEYS - 1) / TT_KEYS;
-  s.groups = (s.n + group_tokens - 1) / group_tokens;
+  s.groups = (s.n + sp.group_tokens - 1) / sp.group_tokens;
+  s.lo = s.g0 = 0;
+  s.hi = s.tiles;
+  if (sp.classes == 2 && s.groups) {
+    if (s.groups == 2) s.g0 = sp.cls;
+    else if (sp.cls == 0) s.hi = (s.tiles + 1) / 2;
+    else s.lo = (s.tiles + 1) / 2;
+    s.groups = 1;
+  }
   return s;
 }
+__device__ __forceinline__ int units_of(const TreeArgs &a, const SeqShape &s) { return (s.hi - s.lo) * s.groups * a.n_kv; }
 // a CTA's walk over its units, one (sequence, group, head) piece after the other; every role keeps its own
 struct Pieces {
-  int b, g, h, kt0, kt1, left, group_tokens;
+  int b, gi, g, h, kt0, kt1, left;
+  Split sp;
   SeqShape s;
-  __device__ __forceinline__ void begin(const TreeArgs &a, int b0, int within, int units, int gt) {
-    group_tokens = gt;
+  __device__ __forceinline__ void begin(const TreeArgs &a, int b0, int within, int units, const Split &split) {
+    sp = split;
     b = b0;
-    s = seq_shape(a, b, gt);
+    s = seq_shape(a, b, sp);
     left = units;
-    kt0 = within % s.tiles;
-    const int item = within / s.tiles;
+    const int len = s.hi - s.lo, item = within / len;
+    kt0 = s.lo + within % len;
     h = item % a.n_kv;
-    g = item / a.n_kv;
-    kt1 = min(s.tiles, kt0 + left);
+    gi = item / a.n_kv;
+    g = s.g0 + gi;
+    kt1 = min(s.hi, kt0 + left);
   }
   __device__ __forceinline__ bool next(const TreeArgs &a) {
     left -= kt1 - kt0;
     if (left <= 0) return false;
     if (++h == a.n_kv) {
       h = 0;
-      if (++g >= s.groups) {
-        g = 0;
-        do { s = seq_shape(a, ++b, group_tokens); } while (s.groups == 0);
+      if (++gi >= s.groups) {
+        gi = 0;
+        do { s = seq_shape(a, ++b, sp); } while (units_of(a, s) == 0);
       }
+      g = s.g0 + gi;
     }
-    kt0 = 0;
-    kt1 = min(s.tiles, left);
+    kt0 = s.lo;
+    kt1 = min(s.hi, kt0 + left);
     return true;
   }
   __device__ __forceinline__ bool whole() const { return kt0 == 0 && kt1 == s.tiles; }
 };
-__device__ __forceinline__ int units_of(const TreeArgs &a, const SeqShape &s) { return s.tiles * s.groups * a.n_kv; }
 
 // 32 visibility bits of keys j0 .. j0 + 31, counted from the first new token (negative: committed), for new token i
 __device__ __forceinline__ uint32_t mask_word(const TreeArgs &a, int t, int i, int n, int w) {
@@ -347,22 +365,12 @@ __device__ __forceinline__ uint32_t sees_word(const TreeArgs &a, int t, int i, i
   return (j0 & 31) ? __funnelshift_r(lo, mask_word(a, t, i, n, (j0 >> 5) + 1), j0 & 31) : lo;
 }
 
-// e4m3 codes as the 16-bit type, exactly: the code's exponent and mantissa bits are those of the wider type with another bias
-__device__ __forceinline__ void widen4(uint32_t codes, uint32_t &lo, uint32_t &hi, bool half) {
-  const uint32_t a = __byte_perm(codes, 0u, 0x1404), b = __byte_perm(codes, 0u, 0x3424);      // two codes in the upper bytes of two halves
-  if (half) {
-    const uint32_t x = (a & 0x80008000u) | ((a >> 1) & 0x3f803f80u), y = (b & 0x80008000u) | ((b >> 1) & 0x3f803f80u);
-    const __half2 f = __float2half2_rn(256.f);
-    const __half2 u = __hmul2(*reinterpret_cast<const __half2 *>(&x), f), v = __hmul2(*reinterpret_cast<const __half2 *>(&y), f);
-    lo = *reinterpret_cast<const uint32_t *>(&u);
-    hi = *reinterpret_cast<const uint32_t *>(&v);
-  } else {
-    const uint32_t x = (a & 0x80008000u) | ((a >> 4) & 0x07f007f0u), y = (b & 0x80008000u) | ((b >> 4) & 0x07f007f0u);
-    const __nv_bfloat162 f = __float2bfloat162_rn(1.329227995784916e36f);      // 2^120
-    const __nv_bfloat162 u = __hmul2(*reinterpret_cast<const __nv_bfloat162 *>(&x), f), v = __hmul2(*reinterpret_cast<const __nv_bfloat162 *>(&y), f);
-    lo = *reinterpret_cast<const uint32_t *>(&u);
-    hi = *reinterpret_cast<const uint32_t *>(&v);
-  }
+// four e4m3 codes as IEEE halves
+__device__ __forceinline__ void widen4(uint32_t codes, uint32_t &lo, uint32_t &hi) {
+  const __half2_raw x = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(codes & 0xffffu), __NV_E4M3);
+  const __half2_raw y = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(codes >> 16), __NV_E4M3);
+  lo = (uint32_t)x.x | (uint32_t)x.y << 16;
+  hi = (uint32_t)y.x | (uint32_t)y.y << 16;
 }
 
 // first cache row of key tile j (a row outside the cache: the tile reads as zeros)
@@ -381,7 +389,7 @@ __global__ void __launch_bounds__(TreeLayout<HD, W, FP8>::THREADS, 1)
 tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                          const __grid_constant__ TreeTcArgs p) {
   using L = TreeLayout<HD, W, FP8>;
-  constexpr bool PV_F16 = F16 && !FP8;          // type of P and V
+  constexpr bool MMA_F16 = F16 || FP8;          // type of the operands: FP8 rows are widened to halves, bf16 queries converted
   const TreeArgs &a = p.a;
   extern __shared__ uint8_t smem_raw[];
   uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -390,15 +398,18 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
   uint64_t *s_full = bars + 5, *p_ready = bars + 7;                              // [2] each
   uint64_t *k_full = bars + 9, *k_empty = k_full + 4, *v_full = k_empty + 4, *v_empty = v_full + 4;      // rings of up to 4
   uint64_t *c_full = v_empty + 4, *c_empty = c_full + 5;                         // rings of up to 5 (FP8 codes)
-  uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(c_empty + 5);
+  uint64_t *q_ready = c_empty + 5, *p_half = q_ready + 1;                        // queries as halves (FP8); [2] first 64 keys of P
+  uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(p_half + 2);
   volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
   volatile int *bad_item = reinterpret_cast<volatile int *>(tmem_slot + 2);      // [2]
   int *start = reinterpret_cast<int *>(tmem_slot + 4);                           // first sequence, units before the range in it
   float2 *ml = reinterpret_cast<float2 *>(smem + L::ML);                         // [item & 1][stream][128]
-  float *scales = reinterpret_cast<float *>(smem + L::SC);                       // [tile & 3][K, V][128]
+  float *scales = reinterpret_cast<float *>(smem + L::SC);                       // [tile & 3][K, V, log2 V][128], then [item & 1][128]
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int group_tokens = W * p.npt, rep = a.n_q / a.n_kv;
+  const int rep = a.n_q / a.n_kv;
+  const Split split{W * p.npt, p.classes, p.classes == 2 ? (int)blockIdx.x & 1 : 0};
+  const int cta = (int)blockIdx.x / p.classes, ctas = ((int)gridDim.x - split.cls + p.classes - 1) / p.classes;      // within the class
 
   // ---- this CTA's range of units: prefix sums over the sequences (in the ring's memory, not yet in use)
   int *warp_sum_s = reinterpret_cast<int *>(smem);
@@ -407,7 +418,7 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
   int mine = 0;
   for (int b = b_lo; b < b_hi; ++b) {
     if (blockIdx.x == 0) { int x, y, z; tree_lengths(a, b, x, y, z, true); }
-    mine += units_of(a, seq_shape(a, b, group_tokens));
+    mine += units_of(a, seq_shape(a, b, split));
   }
   int inc = mine;
 #pragma unroll
@@ -422,13 +433,13 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
     if (w < warp) before += warp_sum_s[w];
     total += warp_sum_s[w];
   }
-  const int per = (total + (int)gridDim.x - 1) / (int)gridDim.x;
-  const int u0 = min((long long)total, (long long)blockIdx.x * per), units = min(total - u0, per);
+  const int per = (total + ctas - 1) / ctas;
+  const int u0 = (int)min((long long)total, (long long)cta * per), units = min(total - u0, per);
   if (units <= 0) return;
   if (u0 >= before && u0 < before + mine) {
     int at = before;
     for (int b = b_lo; b < b_hi; ++b) {
-      const int n = units_of(a, seq_shape(a, b, group_tokens));
+      const int n = units_of(a, seq_shape(a, b, split));
       if (u0 < at + n) { start[0] = b; start[1] = u0 - at; break; }
       at += n;
     }
@@ -443,7 +454,9 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
     for (int s = 0; s < 2; ++s) {
       tc::mbar_init(tc::smem_u32(&s_full[s]), 1);
       tc::mbar_init(tc::smem_u32(&p_ready[s]), 4);
+      tc::mbar_init(tc::smem_u32(&p_half[s]), 4);
     }
+    tc::mbar_init(tc::smem_u32(q_ready), 4);
     for (int s = 0; s < 4; ++s) {
       tc::mbar_init(tc::smem_u32(&k_full[s]), FP8 ? 4 : 1);
       tc::mbar_init(tc::smem_u32(&k_empty[s]), 1);
@@ -468,7 +481,7 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
   const uint32_t tmem_base = *tmem_slot;
   // tensor-memory columns: S0 [0, 128) S1 [128, 256) O0 [256, 256 + HD) O1 [384, 384 + HD); P_w over the first 64 of S_w
   Pieces it;
-  it.begin(a, start[0], start[1], units, group_tokens);
+  it.begin(a, start[0], start[1], units, split);
   auto wait = [&](uint64_t *bar, uint32_t parity) { return tt_wait(tc::smem_u32(bar), parity, abort_flag, a.status); };
 
   if (warp == 0) {
@@ -530,8 +543,8 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
   } else if (warp == 1) {
     // -------------------------------------------------------------------- MMA issuer (one elected lane)
     const bool leader = tc::elect_one();
-    constexpr uint32_t idesc_qk = tc::umma_idesc(128, TT_KEYS, 0, 0, F16, F16);
-    constexpr uint32_t idesc_pv = tc::umma_idesc(128, HD, 0, 1, PV_F16, PV_F16);
+    constexpr uint32_t idesc_qk = tc::umma_idesc(128, TT_KEYS, 0, 0, MMA_F16, MMA_F16);
+    constexpr uint32_t idesc_pv = tc::umma_idesc(128, HD, 0, 1, MMA_F16, MMA_F16);
     const uint64_t q_desc = tc::umma_desc_sw128(tc::smem_u32(smem + L::Q), 16, 1024);
     const uint64_t k_desc = tc::umma_desc_sw128(tc::smem_u32(smem + L::K), 16, 1024);
     const uint64_t v_desc = tc::umma_desc_sw128(tc::smem_u32(smem + L::V), L::CHUNK, 1024);
@@ -560,7 +573,7 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
         if (W == 1 || w == 1) ++kc;
         return true;
       };
-      ok = wait(q_full, item & 1);
+      ok = wait(FP8 ? q_ready : q_full, item & 1);
       tc::tc_fence_after_sync();
       ok = ok && issue_qk(0);
       for (int step = 0; step < steps && ok; ++step) {
@@ -569,15 +582,24 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
         if (W == 1 || w == 0)
           if (!(ok = wait(&v_full[s], (vc / L::VS) & 1))) break;
         if (step == 0 && !(ok = wait(o_empty, (item & 1) ^ 1))) break;
+        // O += P V in two halves: the first 64 keys run while the softmax warps still exponentiate the last 64
         int &sc = w ? sc1 : sc0;
+        const uint64_t vd = v_desc + (uint64_t)(s * (L::TILE >> 4));
+        auto issue_pv = [&](int hf) {
+#pragma unroll
+          for (int k4 = 0; k4 < TT_KEYS / 32; ++k4) {
+            const int kk = hf * (TT_KEYS / 32) + k4;
+            tc::umma_ts(tmem_base + 256 + w * 128, tmem_base + w * 128 + kk * 8, vd + (uint64_t)((kk * 16 * 128) >> 4), idesc_pv, (step > 1 || kk != 0) ? 1u : 0u);
+          }
+        };
+        if (!(ok = wait(&p_half[w], sc & 1))) break;
+        tc::tc_fence_after_sync();
+        if (leader) issue_pv(0);
         if (!(ok = wait(&p_ready[w], sc & 1))) break;
         ++sc;
         tc::tc_fence_after_sync();
         if (leader) {
-          const uint64_t vd = v_desc + (uint64_t)(s * (L::TILE >> 4));
-#pragma unroll
-          for (int kk = 0; kk < TT_KEYS / 16; ++kk)
-            tc::umma_ts(tmem_base + 256 + w * 128, tmem_base + w * 128 + kk * 8, vd + (uint64_t)((kk * 16 * 128) >> 4), idesc_pv, (step > 1 || kk != 0) ? 1u : 0u);
+          issue_pv(1);
           if (W == 1 || w == 1) tc::umma_commit(tc::smem_u32(&v_empty[s]));
           if (step == steps - 1) tc::umma_commit(tc::smem_u32(o_full));
         }
@@ -591,7 +613,9 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
     const int w = (warp - 2) >> 2, quarter = warp & 3, r = quarter * 32 + lane;
     const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
     const uint32_t t_s = tmem_base + lane_base + w * 128, t_o = tmem_base + lane_base + 256;
-    const float c = p.scale_log2;
+    // m_ref in units of the scores (FP8: already in log2 units, c being the row's own)
+    float c = p.scale_log2;
+    const float cm = FP8 ? 1.f : c;
     int item = 0, sc = 0, tc_count = 0;          // tc_count: tiles of earlier pieces (ring positions)
     bool ok = true;
     do {
@@ -637,12 +661,14 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
         if (!(ok = wait(&s_full[w], sc & 1))) break;
         tc::tc_fence_after_sync();
         ++sc;
-        const float *ksc = nullptr, *vsc = nullptr;
+        const float *ksc = nullptr, *vsc = nullptr, *lvs = nullptr;
         if constexpr (FP8) {
-          // (the widening warps wrote both scales of the tile's rows before they announced its V rows)
-          ksc = scales + (tile & 3) * 256;
+          // (the widening warps wrote the scales of the tile's rows before they announced its V rows)
+          ksc = scales + (tile & 3) * 384;
           vsc = ksc + 128;
+          lvs = ksc + 256;
           if (!(ok = wait(&v_full[tile % L::VS], (tile / L::VS) & 1))) break;
+          c = p.scale_log2 * scales[4 * 384 + (item & 1) * 128 + r];         // (written before this piece's first rows)
         }
         if (warp_active) {
           uint32_t words[4] = {0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu};
@@ -679,20 +705,32 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
           for (int hf = 0; hf < 2; ++hf) {
             uint32_t *d = s + (FP8 ? 0 : hf * 64);
             load_half(hf, d);
+            if constexpr (FP8) {
+              // the reference follows the scale-weighted probabilities: s c + log2(V scale)
 #pragma unroll
-            for (int i = 0; i < 64; i += 8) {
-              m0 = tc::max3(m0, __uint_as_float(d[i]), __uint_as_float(d[i + 1]));
-              m1 = tc::max3(m1, __uint_as_float(d[i + 2]), __uint_as_float(d[i + 3]));
-              m2 = tc::max3(m2, __uint_as_float(d[i + 4]), __uint_as_float(d[i + 5]));
-              m3 = tc::max3(m3, __uint_as_float(d[i + 6]), __uint_as_float(d[i + 7]));
+              for (int i = 0; i < 64; i += 4) {
+                const float4 l4 = *reinterpret_cast<const float4 *>(lvs + hf * 64 + i);
+                m0 = fmaxf(m0, fmaf(__uint_as_float(d[i]), c, l4.x));
+                m1 = fmaxf(m1, fmaf(__uint_as_float(d[i + 1]), c, l4.y));
+                m2 = fmaxf(m2, fmaf(__uint_as_float(d[i + 2]), c, l4.z));
+                m3 = fmaxf(m3, fmaf(__uint_as_float(d[i + 3]), c, l4.w));
+              }
+            } else {
+#pragma unroll
+              for (int i = 0; i < 64; i += 8) {
+                m0 = tc::max3(m0, __uint_as_float(d[i]), __uint_as_float(d[i + 1]));
+                m1 = tc::max3(m1, __uint_as_float(d[i + 2]), __uint_as_float(d[i + 3]));
+                m2 = tc::max3(m2, __uint_as_float(d[i + 4]), __uint_as_float(d[i + 5]));
+                m3 = tc::max3(m3, __uint_as_float(d[i + 6]), __uint_as_float(d[i + 7]));
+              }
             }
           }
           const float mx = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3));
-          const bool need = first || (mx - m_ref) * c > TT_RESCALE;
+          const bool need = first || (mx - m_ref) * cm > TT_RESCALE;
           const float m_new = need ? mx : m_ref;
           if (!first && __any_sync(0xffffffffu, need && valid)) {
             // S of this step is complete, so every earlier P V of the stream has retired: O may be rescaled
-            const float f = need ? tt_exp2((m_ref - m_new) * c) : 1.f;
+            const float f = need ? tt_exp2((m_ref - m_new) * cm) : 1.f;
             l *= f;
 #pragma unroll 1
             for (int ch = 0; ch < HD / 16; ++ch) {
@@ -705,7 +743,7 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
             }
           }
           m_ref = m_new;
-          const float neg_mc = m_ref == -INFINITY ? 0.f : -m_ref * c;       // (a row that sees nothing yet: every exponential is 0)
+          const float neg_mc = m_ref == -INFINITY ? 0.f : -m_ref * cm;       // (a row that sees nothing yet: every exponential is 0)
           float l0 = 0.f, l1 = 0.f, l2 = 0.f, l3 = 0.f;
 #pragma unroll
           for (int hf = 0; hf < 2; ++hf) {
@@ -725,18 +763,31 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
                   p0 = (wd & 1u) ? p0 : 0.f; p1 = (wd & 2u) ? p1 : 0.f; p2 = (wd & 4u) ? p2 : 0.f; p3 = (wd & 8u) ? p3 : 0.f;
                 }
               }
-              packed[i / 2] = PV_F16 ? tc::pack_f16x2(p0, p1) : tc::pack_bf16x2(p0, p1);
-              packed[i / 2 + 1] = PV_F16 ? tc::pack_f16x2(p2, p3) : tc::pack_bf16x2(p2, p3);
+              if constexpr (FP8) {                                           // (an infinite scale stays infinite)
+                const __half2 h0 = __floats2half2_rn(p0, p1), h1 = __floats2half2_rn(p2, p3);
+                packed[i / 2] = *reinterpret_cast<const uint32_t *>(&h0);
+                packed[i / 2 + 1] = *reinterpret_cast<const uint32_t *>(&h1);
+              } else {
+                packed[i / 2] = F16 ? tc::pack_f16x2(p0, p1) : tc::pack_bf16x2(p0, p1);
+                packed[i / 2 + 1] = F16 ? tc::pack_f16x2(p2, p3) : tc::pack_bf16x2(p2, p3);
+              }
             }
             tc::tmem_st_32x32b_x32(t_s + hf * 32, packed);      // over scores that have been read for the last time
+            tc::tmem_st_wait();
+            tc::tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(tc::smem_u32(hf ? &p_ready[w] : &p_half[w]));
           }
           l += (l0 + l1) + (l2 + l3);
           first = false;
-          tc::tmem_st_wait();
+        } else {
+          tc::tc_fence_before_sync();
+          __syncwarp();
+          if (lane == 0) {
+            tc::mbar_arrive(tc::smem_u32(&p_half[w]));
+            tc::mbar_arrive(tc::smem_u32(&p_ready[w]));
+          }
         }
-        tc::tc_fence_before_sync();
-        __syncwarp();
-        if (lane == 0) tc::mbar_arrive(tc::smem_u32(&p_ready[w]));
       }
       if (!ok) break;
       // ---- the piece's result.  Both streams meet here once (W = 1: to join their halves of the keys).
@@ -750,21 +801,20 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
         if constexpr (W == 1) {
           const float2 x0 = ml[((item & 1) * 2) * 128 + r], x1 = ml[((item & 1) * 2 + 1) * 128 + r];
           m = fmaxf(x0.x, x1.x);
-          f0 = x0.x == -INFINITY ? 0.f : tt_exp2((x0.x - m) * c);
-          f1 = x1.x == -INFINITY ? 0.f : tt_exp2((x1.x - m) * c);
+          f0 = x0.x == -INFINITY ? 0.f : tt_exp2((x0.x - m) * cm);
+          f1 = x1.x == -INFINITY ? 0.f : tt_exp2((x1.x - m) * cm);
           l = x0.y * f0 + (nt > 1 ? x1.y * f1 : 0.f);
         }
         const bool whole = it.whole(), bad = bad_item[item & 1] == item + 1;
         const float inv = whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
         const size_t head = (size_t)tok * a.n_q + it.h * rep + (valid ? r % rep : 0);
-        const int slot = (int)blockIdx.x * 2 + (it.kt0 == 0 ? 1 : 0);
-        const int srow = (W == 2 ? w : 0) * p.npt * rep + r;
-        float *part = a.scratch + ((size_t)slot * p.slot_rows + srow) * (HD + 2);
+        const int slot = (int)blockIdx.x * 2 + (it.kt0 == it.s.lo ? 1 : 0);
+        const size_t srow = (size_t)slot * p.slot_rows + (W == 2 ? w : 0) * p.npt * rep + r;
         constexpr int COLS = W == 1 ? HD / 2 : HD;
         const int col0 = W == 1 ? w * COLS : 0;
         if (valid && col0 == 0 && (W == 2 || w == 0)) {
-          if (!whole) *reinterpret_cast<float2 *>(part) = make_float2(m * c, l);
-          else if (a.lse) a.lse[head] = l == 0.f ? -INFINITY : m * a.scale + logf(l);
+          if (!whole) reinterpret_cast<float2 *>(a.scratch)[srow] = make_float2(m * cm, l);
+          else if (a.lse) a.lse[head] = l == 0.f ? -INFINITY : m * (cm * 0.6931471805599453f) + logf(l);
         }
 #pragma unroll 1
         for (int ch = 0; ch < COLS / 32; ++ch) {
@@ -818,9 +868,9 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
                 for (int i = 0; i < 32; ++i) dst[i] = (uint16_t)(y[i >> 1] >> ((i & 1) * 16));
               }
             } else {
-              float2 *dst = reinterpret_cast<float2 *>(part + 2 + d0);
+              float *dst = p.part_o + srow * HD + d0;
 #pragma unroll
-              for (int i = 0; i < 16; ++i) dst[i] = make_float2(o[2 * i], o[2 * i + 1]);
+              for (int i = 0; i < 32; i += 8) tc::st_global_v8(dst + i, reinterpret_cast<const uint32_t *>(o) + i);
             }
           }
         }
@@ -832,45 +882,91 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
       ++item;
     } while (it.next(a));
   } else if constexpr (FP8) {
-    // -------------------------------------------------------------------- widening warps: codes -> swizzled 16-bit tiles, scales
+    // -------------------------------------------------------------------- widening warps: codes -> swizzled halves, scales; queries
     const int t = threadIdx.x - 11 * 32;
-    int cc = 0, tile = 0;
+    int cc = 0, tile = 0, item = 0;
     bool ok = true;
     do {
       // a row's scales hang on its page number: the number is asked for two tiles ahead, the scales one
+      const int kv_len = it.s.past + it.s.n;
       auto row_of = [&](int j) {
         const int key = j * TT_KEYS + t;
-        return j < it.kt1 && key < it.s.past + it.s.n ? tree_row(a, it.b, key) : -1;
+        return j < it.kt1 && key < kv_len ? tree_row(a, it.b, key) : -1;
       };
       int row1 = row_of(it.kt0), row2 = row_of(it.kt0 + 1);
       float sk1 = row1 >= 0 ? a.k_scale[row1] : 0.f, sv1 = row1 >= 0 ? a.v_scale[row1] : 0.f;
+      // the query rows, one per thread: times a power of two, bf16 -> half
+      if (!(ok = wait(q_full, item & 1))) break;
+      float back = 1.f;
+      if constexpr (!F16) {
+        uint8_t *qrow = smem + L::Q + t * 128;
+        uint32_t top = 0;
+#pragma unroll 1
+        for (int i = 0; i < L::CHUNKS * 8; ++i) {
+          const uint4 x = *reinterpret_cast<const uint4 *>(qrow + (i >> 3) * L::CHUNK + (i & 7) * 16);
+          const uint32_t xs[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+          for (int q4 = 0; q4 < 4; ++q4) top = max(top, max(xs[q4] & 0x7f80u, (xs[q4] >> 16) & 0x7f80u));
+        }
+        // exponent of the row's maximum -> 14 (a row without finite maximum, and one of zeros: as it is)
+        const int e = (int)(top >> 7);
+        const int shift = e == 0 || e == 255 ? 0 : min(max(14 - (e - 127), -120), 120);
+        const float up = __uint_as_float((uint32_t)(127 + shift) << 23);
+        back = __uint_as_float((uint32_t)(127 - shift) << 23);
+#pragma unroll 1
+        for (int i = 0; i < L::CHUNKS * 8; ++i) {
+          uint4 *at = reinterpret_cast<uint4 *>(qrow + (i >> 3) * L::CHUNK + (i & 7) * 16);
+          const uint4 x = *at;
+          uint32_t xs[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+          for (int q4 = 0; q4 < 4; ++q4) {
+            const __half2 h2 = __floats2half2_rn(__uint_as_float(xs[q4] << 16) * up, __uint_as_float(xs[q4] & 0xffff0000u) * up);
+            xs[q4] = *reinterpret_cast<const uint32_t *>(&h2);
+          }
+          *at = make_uint4(xs[0], xs[1], xs[2], xs[3]);
+        }
+        tc::fence_proxy_async_smem();
+      }
+      scales[4 * 384 + (item & 1) * 128 + t] = back;
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(tc::smem_u32(q_ready));
+      ++item;
       for (int j = it.kt0; j < it.kt1 && ok; ++j, ++tile) {
         const float sk = sk1, sv = sv1;
         sk1 = row2 >= 0 ? a.k_scale[row2] : 0.f;
         sv1 = row2 >= 0 ? a.v_scale[row2] : 0.f;
         row2 = row_of(j + 2);
-        for (int kv = 0; kv < 2 && ok; ++kv, ++cc) {
+        const int live = kv_len - j * TT_KEYS;                 // rows from here on are behind the sequence: zeros
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv, ++cc) {
           const int cs = cc % L::CS, ds = kv ? tile % L::VS : 0;
           const uint8_t *src = smem + L::C + cs * L::CODE_TILE;
           uint8_t *dst = smem + (kv ? L::V : L::K) + ds * L::TILE;
-          ok = wait(&c_full[cs], (cc / L::CS) & 1) && (kv ? wait(&v_empty[ds], ((tile / L::VS) & 1) ^ 1) : wait(&k_empty[0], (tile & 1) ^ 1));
+          ok = ok && wait(&c_full[cs], (cc / L::CS) & 1) && (kv ? wait(&v_empty[ds], ((tile / L::VS) & 1) ^ 1) : wait(&k_empty[0], (tile & 1) ^ 1));
           if (!ok) break;
-          scales[(tile & 3) * 256 + kv * 128 + t] = kv ? sv : sk;
-#pragma unroll 4
-          for (int i = t; i < L::CODE_TILE / 16; i += 128) {
-            const int at = i * 16;
-            const uint4 x = *reinterpret_cast<const uint4 *>(src + at);
-            const int rr = at / HD, col = at % HD;
-            uint4 y0, y1;
-            const bool half = kv ? PV_F16 : F16;
-            widen4(x.x, y0.x, y0.y, half);
-            widen4(x.y, y0.z, y0.w, half);
-            widen4(x.z, y1.x, y1.y, half);
-            widen4(x.w, y1.z, y1.w, half);
-            uint8_t *line = dst + (col >> 6) * L::CHUNK + rr * 128;
-            const int u = (col & 63) >> 3;
-            *reinterpret_cast<uint4 *>(line + (((u) ^ (rr & 7)) << 4)) = y0;
-            *reinterpret_cast<uint4 *>(line + (((u + 1) ^ (rr & 7)) << 4)) = y1;
+          float *sc_t = scales + (tile & 3) * 384;
+          if (kv) {
+            sc_t[128 + t] = sv;
+            sc_t[256 + t] = fminf(fmaxf(__log2f(sv), -126.f), 60.f);      // (beyond 2^60 P itself overflows)
+          } else {
+            sc_t[t] = sk;
+          }
+          // a thread's pieces of 16 codes lie 128 apart: the same columns of rows STEP apart, whose swizzle is the same (STEP % 8 == 0)
+          constexpr int PER_ROW = HD / 16, STEP = 128 / PER_ROW;
+          const int rr0 = t / PER_ROW, col = t % PER_ROW * 16, u = (col & 63) >> 3;
+          uint8_t *line = dst + (col >> 6) * L::CHUNK + rr0 * 128;
+          uint4 *y0 = reinterpret_cast<uint4 *>(line + ((u ^ (rr0 & 7)) << 4)), *y1 = reinterpret_cast<uint4 *>(line + (((u + 1) ^ (rr0 & 7)) << 4));
+          const uint4 *x = reinterpret_cast<const uint4 *>(src) + t;
+#pragma unroll
+          for (int i = 0; i < PER_ROW; ++i) {
+            uint4 c4 = x[i * 128], h0, h1;
+            if (rr0 + i * STEP >= live) c4 = make_uint4(0u, 0u, 0u, 0u);
+            widen4(c4.x, h0.x, h0.y);
+            widen4(c4.y, h0.z, h0.w);
+            widen4(c4.z, h1.x, h1.y);
+            widen4(c4.w, h1.z, h1.w);
+            y0[i * STEP * 8] = h0;
+            y1[i * STEP * 8] = h1;
           }
           tc::fence_proxy_async_smem();
           __syncwarp();
@@ -891,78 +987,111 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
   }
 }
 
-// joins the partial results of the pieces that a (sequence, group, head) was cut into: block per new token
+// joins the partial results of the pieces that a (sequence, group, head) was cut into: block per new token and TJ_THREADS / (HD / 4) heads
 constexpr int TJ_THREADS = 256;
 template <int HD, bool F16>
-__global__ void __launch_bounds__(TJ_THREADS) tree_attention_tc_join_kernel(TreeTcArgs p, int ctas, int tiles_per_group) {
+__global__ void __launch_bounds__(TJ_THREADS) tree_attention_tc_join_kernel(TreeTcArgs p, int grid, int tiles_per_group) {
   const TreeArgs &a = p.a;
   const int t = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int group_tokens = tiles_per_group * p.npt, rep = a.n_q / a.n_kv;
-  __shared__ int s_total[TJ_THREADS / 32], s_before[TJ_THREADS / 32], s_b;
+  __shared__ int s_sum[2][2][TJ_THREADS / 32], s_b;        // [class][before, total]
   if (tid == 0) s_b = -1;
   __syncthreads();
-  int total = 0, before = 0;
+  int sum[2][2] = {{0, 0}, {0, 0}};
   for (int b = tid; b < a.n_seqs; b += TJ_THREADS) {
-    const SeqShape s = seq_shape(a, b, group_tokens);
-    const int u = units_of(a, s);
-    total += u;
-    if (s.tok0 + s.n <= t) before += u;
-    else if (s.tok0 <= t) s_b = b;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      if (k >= p.classes) break;
+      const SeqShape s = seq_shape(a, b, Split{group_tokens, p.classes, k});
+      const int u = units_of(a, s);
+      sum[k][1] += u;
+      if (s.tok0 + s.n <= t) sum[k][0] += u;
+      else if (s.tok0 <= t) s_b = b;
+    }
   }
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    total += __shfl_xor_sync(0xffffffffu, total, o);
-    before += __shfl_xor_sync(0xffffffffu, before, o);
-  }
-  if (lane == 0) { s_total[warp] = total; s_before[warp] = before; }
+  for (int k = 0; k < 2; ++k)
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      int v = sum[k][q];
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+      if (lane == 0) s_sum[k][q][warp] = v;
+    }
   __syncthreads();
   const int b = s_b;
-  if (b < 0) return;                                   // a row behind the last sequence
-  total = before = 0;
-#pragma unroll
-  for (int w = 0; w < TJ_THREADS / 32; ++w) { total += s_total[w]; before += s_before[w]; }
-  const SeqShape s = seq_shape(a, b, group_tokens);
-  const int per = (total + ctas - 1) / ctas;
-  const int node = t - s.tok0, g = node / group_tokens, srow0 = (node - g * group_tokens) * rep;
+  if (b < 0) return;                                       // a row behind the last sequence
   constexpr int LANES = HD / 4, PER_PASS = TJ_THREADS / LANES;
-  const int d = (tid % LANES) * 4;
-  for (int hq = tid / LANES; hq < a.n_q; hq += PER_PASS) {
-    const int h = hq / rep;
-    const int first = before + (g * a.n_kv + h) * s.tiles, last = first + s.tiles - 1;
-    const int c0 = first / per, c1 = last / per;
-    if (c0 == c1) continue;                            // whole: already in `out`
-    const int srow = srow0 + hq % rep;
-    // the first piece starts at the item's first tile: its CTA's slot 1; the others are the first piece of theirs: slot 0
-    auto piece = [&](int ct) { return a.scratch + ((size_t)(ct * 2 + (ct == c0 ? 1 : 0)) * p.slot_rows + srow) * (HD + 2); };
-    float m = -INFINITY;
-#pragma unroll 4
-    for (int ct = c0; ct <= c1; ++ct) m = fmaxf(m, piece(ct)[0]);
-    float l = 0.f, o0 = 0.f, o1 = 0.f, o2 = 0.f, o3 = 0.f;
-#pragma unroll 4
-    for (int ct = c0; ct <= c1; ++ct) {
-      const float *x = piece(ct);
-      const float2 ml = *reinterpret_cast<const float2 *>(x), u = *reinterpret_cast<const float2 *>(x + 2 + d), v = *reinterpret_cast<const float2 *>(x + 4 + d);
-      const float f = ml.x == -INFINITY ? 0.f : tt_exp2(ml.x - m);
-      if (f == 0.f && ml.y == 0.f) continue;           // saw nothing
-      l = fmaf(ml.y, f, l);
-      o0 = fmaf(u.x, f, o0); o1 = fmaf(u.y, f, o1); o2 = fmaf(v.x, f, o2); o3 = fmaf(v.y, f, o3);
-    }
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    if (l == 0.f) o0 = o1 = o2 = o3 = 0.f;
-    const size_t head = (size_t)t * a.n_q + hq;
-    uint16_t y[4];
-    if constexpr (F16) {
-      y[0] = __half_as_ushort(__float2half_rn(o0 * inv)); y[1] = __half_as_ushort(__float2half_rn(o1 * inv));
-      y[2] = __half_as_ushort(__float2half_rn(o2 * inv)); y[3] = __half_as_ushort(__float2half_rn(o3 * inv));
-    } else {
-      y[0] = __bfloat16_as_ushort(__float2bfloat16_rn(o0 * inv)); y[1] = __bfloat16_as_ushort(__float2bfloat16_rn(o1 * inv));
-      y[2] = __bfloat16_as_ushort(__float2bfloat16_rn(o2 * inv)); y[3] = __bfloat16_as_ushort(__float2bfloat16_rn(o3 * inv));
-    }
-    uint16_t *dst = reinterpret_cast<uint16_t *>(a.out) + head * HD + d;
-    if (p.store32) *reinterpret_cast<uint2 *>(dst) = make_uint2((uint32_t)y[0] | (uint32_t)y[1] << 16, (uint32_t)y[2] | (uint32_t)y[3] << 16);
-    else { dst[0] = y[0]; dst[1] = y[1]; dst[2] = y[2]; dst[3] = y[3]; }
-    if (a.lse && d == 0) a.lse[head] = l == 0.f ? -INFINITY : m * 0.6931471805599453f + logf(l);
+  const int d = (tid % LANES) * 4, hq = blockIdx.y * PER_PASS + tid / LANES, h = hq / rep;
+  if (hq >= a.n_q) return;
+  // the CTAs of each class that worked on this row's item, in the order of the keys
+  int c0[2], n_pieces[2] = {0, 0}, row = 0;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    c0[k] = 0;
+    if (k >= p.classes) break;
+    const SeqShape s = seq_shape(a, b, Split{group_tokens, p.classes, k});
+    const int node = t - s.tok0, g = node / group_tokens, len = s.hi - s.lo;
+    row = (node - g * group_tokens) * rep + hq % rep;
+    if (g < s.g0 || g >= s.g0 + s.groups || len == 0) continue;
+    int before = 0, total = 0;
+#pragma unroll
+    for (int w = 0; w < TJ_THREADS / 32; ++w) { before += s_sum[k][0][w]; total += s_sum[k][1][w]; }
+    const int ctas = (grid - k + p.classes - 1) / p.classes, per = (total + ctas - 1) / ctas;
+    const int first = before + ((g - s.g0) * a.n_kv + h) * len;
+    c0[k] = first / per;
+    n_pieces[k] = (first + len - 1) / per - c0[k] + 1;
   }
+  const int n = n_pieces[0] + n_pieces[1];
+  if (n <= 1) return;                                      // whole: already in `out`
+  // a class's first piece starts at its first key: its CTA's slot 1; the others are the first piece of theirs: slot 0
+  auto piece = [&](int i) -> size_t {
+    const int k = i < n_pieces[0] ? 0 : 1, j = k ? i - n_pieces[0] : i;
+    return (size_t)((((c0[k] + j) * p.classes + k) * 2 + (j == 0 ? 1 : 0))) * p.slot_rows + row;
+  };
+  const float2 *ml = reinterpret_cast<const float2 *>(a.scratch);
+  float m = -INFINITY, l = 0.f, o0 = 0.f, o1 = 0.f, o2 = 0.f, o3 = 0.f;
+  for (int i0 = 0; i0 < n; i0 += 4) {                      // four pieces in flight
+    float2 x[4];
+    float4 u[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      x[q] = make_float2(-INFINITY, 0.f);
+      if (i0 + q < n) {
+        const size_t at = piece(i0 + q);
+        x[q] = ml[at];
+        u[q] = *reinterpret_cast<const float4 *>(p.part_o + at * HD + d);
+      }
+    }
+    float m_new = m;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) m_new = fmaxf(m_new, x[q].x);
+    const float back = m == -INFINITY ? 0.f : tt_exp2(m - m_new);
+    l *= back; o0 *= back; o1 *= back; o2 *= back; o3 *= back;
+    m = m_new;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const float f = x[q].x == -INFINITY ? 0.f : tt_exp2(x[q].x - m);
+      if (f == 0.f && x[q].y == 0.f) continue;             // saw nothing
+      l = fmaf(x[q].y, f, l);
+      o0 = fmaf(u[q].x, f, o0); o1 = fmaf(u[q].y, f, o1); o2 = fmaf(u[q].z, f, o2); o3 = fmaf(u[q].w, f, o3);
+    }
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  if (l == 0.f) o0 = o1 = o2 = o3 = 0.f;
+  const size_t head = (size_t)t * a.n_q + hq;
+  uint16_t y[4];
+  if constexpr (F16) {
+    y[0] = __half_as_ushort(__float2half_rn(o0 * inv)); y[1] = __half_as_ushort(__float2half_rn(o1 * inv));
+    y[2] = __half_as_ushort(__float2half_rn(o2 * inv)); y[3] = __half_as_ushort(__float2half_rn(o3 * inv));
+  } else {
+    y[0] = __bfloat16_as_ushort(__float2bfloat16_rn(o0 * inv)); y[1] = __bfloat16_as_ushort(__float2bfloat16_rn(o1 * inv));
+    y[2] = __bfloat16_as_ushort(__float2bfloat16_rn(o2 * inv)); y[3] = __bfloat16_as_ushort(__float2bfloat16_rn(o3 * inv));
+  }
+  uint16_t *dst = reinterpret_cast<uint16_t *>(a.out) + head * HD + d;
+  if (p.store32) *reinterpret_cast<uint2 *>(dst) = make_uint2((uint32_t)y[0] | (uint32_t)y[1] << 16, (uint32_t)y[2] | (uint32_t)y[3] << 16);
+  else { dst[0] = y[0]; dst[1] = y[1]; dst[2] = y[2]; dst[3] = y[3]; }
+  if (a.lse && d == 0) a.lse[head] = l == 0.f ? -INFINITY : m * 0.6931471805599453f + logf(l);
 }
 
 // rows of a partial result: those of a group of query tiles, or all that a call has for one KV head
@@ -972,7 +1101,7 @@ int tc_slot_rows(int total_new, int n_q, int n_kv) {
 }
 size_t tc_scratch(int total_new, int n_q, int hd) {
   // (independent of the group size: a call's rows of one KV head are at most all its rows)
-  return (size_t)num_sms() * 2 * tc_slot_rows(total_new, n_q, 1) * (hd + 2) * sizeof(float);
+  return (size_t)num_sms() * 2 * tc_slot_rows(total_new, n_q, 1) * (hd + 2) * sizeof(float) + 256;
 }
 
 // shapes and addresses that the tensor-core form takes (TMA: 16-byte boundaries and strides)
@@ -983,7 +1112,7 @@ bool tc_supported(const TreeArgs &a, bool q16, bool fp8) {
 }
 
 template <int HD, int W, bool F16, bool FP8>
-int32_t launch_tc(const TreeTcArgs &p, int max_kv, cudaStream_t st) {
+int32_t launch_tc(TreeTcArgs p, int max_kv, cudaStream_t st) {
   using L = TreeLayout<HD, W, FP8>;
   static_assert(L::BYTES <= 232448, "shared memory of one CTA");
   const TreeArgs &a = p.a;
@@ -1000,10 +1129,14 @@ int32_t launch_tc(const TreeTcArgs &p, int max_kv, cudaStream_t st) {
   const long long most = groups * tiles * a.n_kv * a.n_seqs;
   if (most > 0x7fffffffLL) return report_error(SWIFTKV_ERR_UNSUPPORTED, "too many key tiles for one launch");
   const int grid = (int)(most < num_sms() ? most : num_sms());
+  p.classes = groups == 2 && grid > 1 ? 2 : 1;
+  const size_t ml_bytes = ((size_t)grid * 2 * p.slot_rows * sizeof(float2) + 255) & ~(size_t)255;
+  p.part_o = reinterpret_cast<float *>(reinterpret_cast<uint8_t *>(a.scratch) + ml_bytes);
   kernel<<<grid, L::THREADS, L::BYTES, st>>>(tq, tk, tv, p);
   cudaError_t e = cudaGetLastError();
   if (e == cudaSuccess && grid > 1) {
-    tree_attention_tc_join_kernel<HD, F16><<<a.total_new, TJ_THREADS, 0, st>>>(p, grid, W);
+    constexpr int PER_PASS = TJ_THREADS / (HD / 4);
+    tree_attention_tc_join_kernel<HD, F16><<<dim3(a.total_new, (a.n_q + PER_PASS - 1) / PER_PASS), TJ_THREADS, 0, st>>>(p, grid, W);
     e = cudaGetLastError();
   }
   return e == cudaSuccess ? SWIFTKV_OK : report_error(SWIFTKV_ERR_CUDA, cudaGetErrorString(e));
@@ -1055,7 +1188,7 @@ extern "C" int32_t swiftkv_tree_attention(const void *q, int64_t q_stride, int32
   if (fp8 ? (!k_scale || !v_scale) : (k_scale || v_scale)) return report_error(SWIFTKV_ERR_INVALID_ARG, "row scales go with an FP8 cache, and with it alone");
   if (!(softmax_scale >= 0.f) || !(softmax_scale < INFINITY)) return report_error(SWIFTKV_ERR_INVALID_ARG, "softmax_scale must be finite and not negative");
   const uintptr_t es = q_dtype == SWIFTKV_DTYPE_F32 ? 4 : 2, kes = fp8 ? 1 : es;
-  if ((uintptr_t)q % es || (uintptr_t)out % es || (uintptr_t)k_cache % kes || (uintptr_t)v_cache % kes || ((uintptr_t)scratch & 15))
+  if ((uintptr_t)q % es || (uintptr_t)out % es || (uintptr_t)k_cache % kes || (uintptr_t)v_cache % kes || ((uintptr_t)scratch & 255))
     return report_error(SWIFTKV_ERR_INVALID_ARG, "misaligned pointer");
   const size_t need = swiftkv_tree_attention_scratch_bytes(total_new, max_kv, n_q_heads, head_dim);
   if (need && (!scratch || scratch_bytes < need)) return report_error(SWIFTKV_ERR_WORKSPACE_SMALL, "scratch too small (see swiftkv_tree_attention_scratch_bytes)");
