@@ -25,6 +25,10 @@
 namespace skv {
 namespace {
 namespace cg = cooperative_groups;
+using tc::F2;
+using tc::add2;
+using tc::fma2;
+using tc::max_nan;
 
 constexpr int LP_THREADS = 256, LP_WARPS = LP_THREADS / 32;     // threads that read logits; one more warp joins up
 constexpr int LP_MAX_TOP = 32;
@@ -36,11 +40,6 @@ constexpr int LP_SMEM = LP_STAGES * LP_CHUNK * 16;
 constexpr float LP_RESCALE = 16.f;           // the reference moves when the sums could grow by more than 2^16
 constexpr float LOWEST = -3.0e38f;
 
-__device__ __forceinline__ float max_nan(float a, float b) {
-  float r;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-  return r;
-}
 __device__ __forceinline__ float exp2_approx(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -92,19 +91,6 @@ __device__ __forceinline__ float lp_load(const __half *p) { return __half2float(
 __device__ __forceinline__ void lp_store(float *p, float v) { *p = v; }
 __device__ __forceinline__ void lp_store(bf16 *p, float v) { *p = __float2bfloat16_rn(v); }
 __device__ __forceinline__ void lp_store(__half *p, float v) { *p = __float2half_rn(v); }
-
-// two fp32 operations per instruction
-union F2 { float f[2]; unsigned long long u; };
-__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
-  F2 r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.u) : "l"(a.u), "l"(b.u), "l"(c.u));
-  return r;
-}
-__device__ __forceinline__ F2 add2(F2 a, F2 b) {
-  F2 r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.u) : "l"(a.u), "l"(b.u));
-  return r;
-}
 
 // whole-number keys in the order of the values (NaN above all); 0 stands for "no element"
 __device__ __forceinline__ uint32_t order_key(float x) {

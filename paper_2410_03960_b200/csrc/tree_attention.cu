@@ -260,7 +260,7 @@ struct TreeLayout {
   static constexpr int ML = SC + (FP8 ? (4 * 3 + 2) * 128 * 4 : 0); // scales: 4 tiles x (K, V, log2 V) x 128; query rows' powers of two x 2
   static constexpr int BAR = ML + 2 * 2 * 128 * 8;                  // (m, l) of both streams, two items
   static constexpr int BYTES = BAR + 512 + 1024;
-  static constexpr int WARPS = 11 + (FP8 ? 4 : 0);
+  static constexpr int WARPS = 10 + (FP8 ? 4 : 0);       // copies, MMA, softmax of two streams, widening
   static constexpr int THREADS = WARPS * 32;
 };
 
@@ -392,14 +392,14 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
   constexpr bool MMA_F16 = F16 || FP8;          // type of the operands: FP8 rows are widened to halves, bf16 queries converted
   const TreeArgs &a = p.a;
   extern __shared__ uint8_t smem_raw[];
-  uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  uint8_t *smem = smem_raw + (-tc::smem_u32(smem_raw) & 1023u);        // (an offset, so that accesses stay known as shared-memory ones)
   uint64_t *bars = reinterpret_cast<uint64_t *>(smem + L::BAR);
-  uint64_t *q_full = bars, *q_empty = bars + 1, *o_full = bars + 2, *o_empty = bars + 3, *x_full = bars + 4;
-  uint64_t *s_full = bars + 5, *p_ready = bars + 7;                              // [2] each
+  uint64_t *q_full = bars, *o_full = bars + 2, *o_empty = bars + 3, *x_full = bars + 4;
+  uint64_t *s_full = bars + 5, *s_half = bars + 7;                               // [2] each: all of S, its first 64 keys
   uint64_t *k_full = bars + 9, *k_empty = k_full + 4, *v_full = k_empty + 4, *v_empty = v_full + 4;      // rings of up to 4
   uint64_t *c_full = v_empty + 4, *c_empty = c_full + 5;                         // rings of up to 5 (FP8 codes)
-  uint64_t *q_ready = c_empty + 5, *p_half = q_ready + 1;                        // queries as halves (FP8); [2] first 64 keys of P
-  uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(p_half + 2);
+  uint64_t *q_ready = c_empty + 5, *p_part = q_ready + 1;                        // queries as halves (FP8); [half of the keys][stream] P
+  uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(p_part + 4);
   volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
   volatile int *bad_item = reinterpret_cast<volatile int *>(tmem_slot + 2);      // [2]
   int *start = reinterpret_cast<int *>(tmem_slot + 4);                           // first sequence, units before the range in it
@@ -447,14 +447,14 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
 
   if (threadIdx.x == 0) {
     tc::mbar_init(tc::smem_u32(q_full), 1);
-    tc::mbar_init(tc::smem_u32(q_empty), 1);
     tc::mbar_init(tc::smem_u32(o_full), 1);
     tc::mbar_init(tc::smem_u32(o_empty), 8);
     tc::mbar_init(tc::smem_u32(x_full), 8);
     for (int s = 0; s < 2; ++s) {
       tc::mbar_init(tc::smem_u32(&s_full[s]), 1);
-      tc::mbar_init(tc::smem_u32(&p_ready[s]), 4);
-      tc::mbar_init(tc::smem_u32(&p_half[s]), 4);
+      tc::mbar_init(tc::smem_u32(&p_part[s]), 4);
+      tc::mbar_init(tc::smem_u32(&p_part[2 + s]), 4);
+      tc::mbar_init(tc::smem_u32(&s_half[s]), 1);
     }
     tc::mbar_init(tc::smem_u32(q_ready), 4);
     for (int s = 0; s < 4; ++s) {
@@ -526,30 +526,24 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
         row = tile_row(a, it.b, it.kt0);
       } while (true);
     }
-  } else if (warp == 10) {
-    if (lane == 0) {
-      // ------------------------------------------------------------------ query tiles, as soon as the last piece's Q K^T are done
-      int item = 0;
-      do {
-        if (!wait(q_empty, (item & 1) ^ 1)) break;
-        const uint32_t bar = tc::smem_u32(q_full);
-        tc::mbar_expect_tx(bar, W * L::CHUNKS * p.npt * rep * 128);
-        for (int w = 0; w < W; ++w)
-          for (int c = 0; c < L::CHUNKS; ++c)
-            tc::tma_load_3d(tc::smem_u32(smem + L::Q + w * L::TILE + c * L::CHUNK), &tmQ, bar, c * 64, it.h * rep, it.s.tok0 + (it.g * W + w) * p.npt);
-        ++item;
-      } while (it.next(a));
-    }
   } else if (warp == 1) {
-    // -------------------------------------------------------------------- MMA issuer (one elected lane)
+    // -------------------------------------------------------------------- MMA issuer (one elected lane), query tiles
     const bool leader = tc::elect_one();
-    constexpr uint32_t idesc_qk = tc::umma_idesc(128, TT_KEYS, 0, 0, MMA_F16, MMA_F16);
+    constexpr uint32_t idesc_qk = tc::umma_idesc(128, TT_KEYS / 2, 0, 0, MMA_F16, MMA_F16);
     constexpr uint32_t idesc_pv = tc::umma_idesc(128, HD, 0, 1, MMA_F16, MMA_F16);
     const uint64_t q_desc = tc::umma_desc_sw128(tc::smem_u32(smem + L::Q), 16, 1024);
     const uint64_t k_desc = tc::umma_desc_sw128(tc::smem_u32(smem + L::K), 16, 1024);
     const uint64_t v_desc = tc::umma_desc_sw128(tc::smem_u32(smem + L::V), L::CHUNK, 1024);
     int kc = 0, vc = 0, item = 0, sc0 = 0, sc1 = 0;
-    bool ok = true;
+    bool ok = true, more;
+    auto load_q = [&]() {
+      const uint32_t bar = tc::smem_u32(q_full);
+      tc::mbar_expect_tx(bar, W * L::CHUNKS * p.npt * rep * 128);
+      for (int w = 0; w < W; ++w)
+        for (int c = 0; c < L::CHUNKS; ++c)
+          tc::tma_load_3d(tc::smem_u32(smem + L::Q + w * L::TILE + c * L::CHUNK), &tmQ, bar, c * 64, it.h * rep, it.s.tok0 + (it.g * W + w) * p.npt);
+    };
+    if (leader) load_q();
     do {
       const int nt = it.kt1 - it.kt0, steps = W == 2 ? 2 * nt : nt;
       // S of a step; steps alternate between the streams.  The stream's last P V was issued before, and runs before.
@@ -560,15 +554,18 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
           tc::tc_fence_after_sync();
         }
         if (leader) {
+          // the scores of 64 keys after the other 64: the softmax warps start on the first half
           const uint64_t qd = q_desc + (uint64_t)((W == 2 ? w : 0) * (L::TILE >> 4)), kd = k_desc + (uint64_t)(s * (L::TILE >> 4));
 #pragma unroll
-          for (int kk = 0; kk < HD / 16; ++kk) {
-            const uint32_t off = ((kk >> 2) * L::CHUNK + (kk & 3) * 32) >> 4;
-            tc::umma_ss(tmem_base + w * 128, qd + off, kd + off, idesc_qk, kk != 0);
+          for (int hf = 0; hf < 2; ++hf) {
+#pragma unroll
+            for (int kk = 0; kk < HD / 16; ++kk) {
+              const uint32_t off = ((kk >> 2) * L::CHUNK + (kk & 3) * 32) >> 4;
+              tc::umma_ss(tmem_base + w * 128 + hf * 64, qd + off, kd + off + hf * (64 * 128 >> 4), idesc_qk, kk != 0);
+            }
+            tc::umma_commit(tc::smem_u32(hf ? &s_full[w] : &s_half[w]));
           }
-          tc::umma_commit(tc::smem_u32(&s_full[w]));
           if (W == 1 || w == 1) tc::umma_commit(tc::smem_u32(&k_empty[s]));
-          if (step == steps - 1) tc::umma_commit(tc::smem_u32(q_empty));
         }
         if (W == 1 || w == 1) ++kc;
         return true;
@@ -582,24 +579,24 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
         if (W == 1 || w == 0)
           if (!(ok = wait(&v_full[s], (vc / L::VS) & 1))) break;
         if (step == 0 && !(ok = wait(o_empty, (item & 1) ^ 1))) break;
-        // O += P V in two halves: the first 64 keys run while the softmax warps still exponentiate the last 64
+        // O += P V in two halves of 64 keys, in the order in which the softmax warps finish them
+        constexpr int FIRST = FP8 ? 0 : 1;
         int &sc = w ? sc1 : sc0;
         const uint64_t vd = v_desc + (uint64_t)(s * (L::TILE >> 4));
-        auto issue_pv = [&](int hf) {
+        auto issue_pv = [&](int hf, bool accumulate) {
 #pragma unroll
-          for (int k4 = 0; k4 < TT_KEYS / 32; ++k4) {
-            const int kk = hf * (TT_KEYS / 32) + k4;
-            tc::umma_ts(tmem_base + 256 + w * 128, tmem_base + w * 128 + kk * 8, vd + (uint64_t)((kk * 16 * 128) >> 4), idesc_pv, (step > 1 || kk != 0) ? 1u : 0u);
-          }
+          for (int k4 = 0; k4 < TT_KEYS / 32; ++k4)
+            tc::umma_ts(tmem_base + 256 + w * 128, tmem_base + w * 128 + hf * 64 + k4 * 8, vd + (uint64_t)(((hf * 4 + k4) * 16 * 128) >> 4), idesc_pv,
+                        (accumulate || k4 != 0) ? 1u : 0u);
         };
-        if (!(ok = wait(&p_half[w], sc & 1))) break;
+        if (!(ok = wait(&p_part[FIRST * 2 + w], sc & 1))) break;
         tc::tc_fence_after_sync();
-        if (leader) issue_pv(0);
-        if (!(ok = wait(&p_ready[w], sc & 1))) break;
+        if (leader) issue_pv(FIRST, step > 1);
+        if (!(ok = wait(&p_part[(1 - FIRST) * 2 + w], sc & 1))) break;
         ++sc;
         tc::tc_fence_after_sync();
         if (leader) {
-          issue_pv(1);
+          issue_pv(1 - FIRST, true);
           if (W == 1 || w == 1) tc::umma_commit(tc::smem_u32(&v_empty[s]));
           if (step == steps - 1) tc::umma_commit(tc::smem_u32(o_full));
         }
@@ -607,7 +604,10 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
       }
       ++item;
       __syncwarp();
-    } while (ok && it.next(a));
+      // the next piece's queries: every Q K^T of this one has retired (its last P came from it), so their place is free
+      more = ok && it.next(a);
+      if (more && leader) load_q();
+    } while (more);
   } else if (warp < 10) {
     // -------------------------------------------------------------------- softmax: stream w, a query row per thread
     const int w = (warp - 2) >> 2, quarter = warp & 3, r = quarter * 32 + lane;
@@ -658,136 +658,176 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
             }
           }
         }
-        if (!(ok = wait(&s_full[w], sc & 1))) break;
+        if (!(ok = wait(FP8 ? &s_full[w] : &s_half[w], sc & 1))) break;
         tc::tc_fence_after_sync();
-        ++sc;
-        const float *ksc = nullptr, *vsc = nullptr, *lvs = nullptr;
+        // (the widening warps wrote the scales of the tile's rows before they announced its V rows)
+        const float4 *ksc = reinterpret_cast<const float4 *>(scales + (tile & 3) * 384), *vsc = ksc + 32, *lvs = ksc + 64;
         if constexpr (FP8) {
-          // (the widening warps wrote the scales of the tile's rows before they announced its V rows)
-          ksc = scales + (tile & 3) * 384;
-          vsc = ksc + 128;
-          lvs = ksc + 256;
           if (!(ok = wait(&v_full[tile % L::VS], (tile / L::VS) & 1))) break;
           c = p.scale_log2 * scales[4 * 384 + (item & 1) * 128 + r];         // (written before this piece's first rows)
         }
         if (warp_active) {
-          uint32_t words[4] = {0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu};
-          if (edge) {
+          // moves the reference to mx where the row outgrew it; S of this step is complete, so every earlier P V of the stream has
+          // retired and O may be rescaled
+          auto refer = [&](float mx) {
+            const bool need = first || (mx - m_ref) * cm > TT_RESCALE;
+            const float m_new = need ? mx : m_ref;
+            if (!first && __any_sync(0xffffffffu, need && valid)) {
+              const float f = need ? tt_exp2((m_ref - m_new) * cm) : 1.f;
+              l *= f;
+#pragma unroll 1
+              for (int ch = 0; ch < HD / 16; ++ch) {
+                uint32_t o[16];
+                tc::tmem_ld_32x32b_x16(t_o + w * 128 + ch * 16, o);
+                tc::tmem_ld_wait();
 #pragma unroll
-            for (int q4 = 0; q4 < 4; ++q4) words[q4] = valid ? sees_word(a, tok, node, it.s.n, j0 + 32 * q4) : 0u;
-          }
-          // scores in 64-column halves; kept in registers between the maximum and the exponentials, except with an FP8 cache, whose
-          // four more warps leave no room: there they are read twice
-          constexpr int KEEP = FP8 ? 64 : 128;
-          uint32_t s[KEEP];
-          auto load_half = [&](int hf, uint32_t *d) {
-            tc::tmem_ld_32x32b_x32p(t_s + hf * 64, d);
-            tc::tmem_ld_32x32b_x32p(t_s + hf * 64 + 32, d + 32);
+                for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                tc::tmem_st_32x32b_x16(t_o + w * 128 + ch * 16, o);
+              }
+            }
+            m_ref = m_new;
+            first = false;
+          };
+          auto announce = [&](int hf) {                                       // 64 keys of P (half hf) are in tensor memory
+            tc::tmem_st_wait();
+            tc::tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(tc::smem_u32(&p_part[hf * 2 + w]));
+          };
+          if constexpr (!FP8) {
+            // Scores in four chunks of 32 columns.  All four give the maximum; chunks 2 and 3 stay in registers and are exponentiated
+            // first, chunks 0 and 1 are read again (128 scores in registers would spill, and spilled registers live in L2: shared
+            // memory leaves L1 next to nothing).  P of keys 64 .. 127 goes over chunk 2, that of 0 .. 63 over chunk 0.
+            auto mask = [&](uint32_t (&d)[32], int ch) {
+              if (!edge) return;
+              const uint32_t seen = valid ? sees_word(a, tok, node, it.s.n, j0 + ch * 32) : 0u;
+#pragma unroll
+              for (int i = 0; i < 32; ++i)
+                if (!((seen >> i) & 1u)) d[i] = 0xff800000u;      // -inf
+            };
+            float m0 = -INFINITY, m1 = -INFINITY;
+            auto maximum = [&](const uint32_t (&d)[32]) {
+#pragma unroll
+              for (int i = 0; i < 32; i += 4) {
+                m0 = tc::max3(m0, __uint_as_float(d[i]), __uint_as_float(d[i + 1]));
+                m1 = tc::max3(m1, __uint_as_float(d[i + 2]), __uint_as_float(d[i + 3]));
+              }
+            };
+            uint32_t u[32], v[32];
+            tc::tmem_ld_32x32b_x32(t_s, u);
+            tc::tmem_ld_32x32b_x32(t_s + 32, v);
             tc::tmem_ld_wait();
-            if constexpr (FP8) {
+            mask(u, 0);
+            mask(v, 1);
+            maximum(u);
+            maximum(v);
+            if (!(ok = wait(&s_full[w], sc & 1))) break;
+            tc::tc_fence_after_sync();
+            tc::tmem_ld_32x32b_x32(t_s + 64, u);
+            tc::tmem_ld_32x32b_x32(t_s + 96, v);
+            tc::tmem_ld_wait();
+            mask(u, 2);
+            mask(v, 3);
+            maximum(u);
+            maximum(v);
+            refer(fmaxf(m0, m1));
+            const float neg_mc = m_ref == -INFINITY ? 0.f : -m_ref * cm;      // (a row that sees nothing yet: every exponential is 0)
+            tc::F2 la{{0.f, 0.f}}, lb{{0.f, 0.f}};
+            const tc::F2 c2{{c, c}}, n2{{neg_mc, neg_mc}};
+            auto exponentials = [&](const uint32_t (&d)[32], int ch) {
+              uint32_t packed[16];
 #pragma unroll
-              for (int i = 0; i < 64; i += 4) {
-                const float4 k4 = *reinterpret_cast<const float4 *>(ksc + hf * 64 + i);
+              for (int i = 0; i < 16; ++i) {
+                tc::F2 x = tc::fma2(tc::F2{{__uint_as_float(d[2 * i]), __uint_as_float(d[2 * i + 1])}}, c2, n2);
+                x = tc::F2{{tt_exp2(x.f[0]), tt_exp2(x.f[1])}};
+                if (i & 1) lb = tc::add2(lb, x); else la = tc::add2(la, x);
+                packed[i] = F16 ? tc::pack_f16x2(x.f[0], x.f[1]) : tc::pack_bf16x2(x.f[0], x.f[1]);
+              }
+              tc::tmem_st_32x32b_x16(t_s + (ch >> 1) * 64 + (ch & 1) * 16, packed);
+            };
+            exponentials(u, 2);
+            tc::tmem_ld_32x32b_x32(t_s, u);
+            exponentials(v, 3);
+            announce(1);
+            tc::tmem_ld_32x32b_x32(t_s + 32, v);
+            tc::tmem_ld_wait();
+            mask(u, 0);
+            mask(v, 1);
+            exponentials(u, 0);
+            exponentials(v, 1);
+            announce(0);
+            l += (la.f[0] + la.f[1]) + (lb.f[0] + lb.f[1]);
+          } else {
+            // 32 columns at a time, once for the maximum and once for the exponentials: scores times the row scales of K
+            auto load = [&](int ch, uint32_t (&d)[32], uint32_t &seen) {
+              tc::tmem_ld_32x32b_x32(t_s + ch * 32, d);
+              seen = !edge ? 0xffffffffu : valid ? sees_word(a, tok, node, it.s.n, j0 + ch * 32) : 0u;
+              tc::tmem_ld_wait();
+#pragma unroll
+              for (int i = 0; i < 32; i += 4) {
+                const float4 k4 = ksc[ch * 8 + i / 4];
                 d[i] = __float_as_uint(__uint_as_float(d[i]) * k4.x);
                 d[i + 1] = __float_as_uint(__uint_as_float(d[i + 1]) * k4.y);
                 d[i + 2] = __float_as_uint(__uint_as_float(d[i + 2]) * k4.z);
                 d[i + 3] = __float_as_uint(__uint_as_float(d[i + 3]) * k4.w);
               }
-            }
-            if (edge) {
+              if (seen != 0xffffffffu) {
 #pragma unroll
-              for (int i = 0; i < 64; ++i)
-                if (!((words[hf * 2 + (i >> 5)] >> (i & 31)) & 1u)) d[i] = 0xff800000u;      // -inf
-            }
-          };
-          float m0 = -INFINITY, m1 = -INFINITY, m2 = -INFINITY, m3 = -INFINITY;
-#pragma unroll
-          for (int hf = 0; hf < 2; ++hf) {
-            uint32_t *d = s + (FP8 ? 0 : hf * 64);
-            load_half(hf, d);
-            if constexpr (FP8) {
+                for (int i = 0; i < 32; ++i)
+                  if (!((seen >> i) & 1u)) d[i] = 0xff800000u;      // -inf
+              }
+            };
+            uint32_t d[32], seen;
+            float m0 = -INFINITY, m1 = -INFINITY, m2 = -INFINITY, m3 = -INFINITY;
+#pragma unroll 1
+            for (int ch = 0; ch < 4; ++ch) {
+              load(ch, d, seen);
               // the reference follows the scale-weighted probabilities: s c + log2(V scale)
 #pragma unroll
-              for (int i = 0; i < 64; i += 4) {
-                const float4 l4 = *reinterpret_cast<const float4 *>(lvs + hf * 64 + i);
+              for (int i = 0; i < 32; i += 4) {
+                const float4 l4 = lvs[ch * 8 + i / 4];
                 m0 = fmaxf(m0, fmaf(__uint_as_float(d[i]), c, l4.x));
                 m1 = fmaxf(m1, fmaf(__uint_as_float(d[i + 1]), c, l4.y));
                 m2 = fmaxf(m2, fmaf(__uint_as_float(d[i + 2]), c, l4.z));
                 m3 = fmaxf(m3, fmaf(__uint_as_float(d[i + 3]), c, l4.w));
               }
-            } else {
-#pragma unroll
-              for (int i = 0; i < 64; i += 8) {
-                m0 = tc::max3(m0, __uint_as_float(d[i]), __uint_as_float(d[i + 1]));
-                m1 = tc::max3(m1, __uint_as_float(d[i + 2]), __uint_as_float(d[i + 3]));
-                m2 = tc::max3(m2, __uint_as_float(d[i + 4]), __uint_as_float(d[i + 5]));
-                m3 = tc::max3(m3, __uint_as_float(d[i + 6]), __uint_as_float(d[i + 7]));
-              }
             }
-          }
-          const float mx = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3));
-          const bool need = first || (mx - m_ref) * cm > TT_RESCALE;
-          const float m_new = need ? mx : m_ref;
-          if (!first && __any_sync(0xffffffffu, need && valid)) {
-            // S of this step is complete, so every earlier P V of the stream has retired: O may be rescaled
-            const float f = need ? tt_exp2((m_ref - m_new) * cm) : 1.f;
-            l *= f;
+            refer(fmaxf(fmaxf(m0, m1), fmaxf(m2, m3)));
+            const float neg_mc = m_ref == -INFINITY ? 0.f : -m_ref;
+            float l0 = 0.f, l1 = 0.f, l2 = 0.f, l3 = 0.f;
 #pragma unroll 1
-            for (int ch = 0; ch < HD / 16; ++ch) {
-              uint32_t o[16];
-              tc::tmem_ld_32x32b_x16(t_o + w * 128 + ch * 16, o);
-              tc::tmem_ld_wait();
+            for (int ch = 0; ch < 4; ++ch) {
+              load(ch, d, seen);
+              uint32_t packed[16];
 #pragma unroll
-              for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-              tc::tmem_st_32x32b_x16(t_o + w * 128 + ch * 16, o);
-            }
-          }
-          m_ref = m_new;
-          const float neg_mc = m_ref == -INFINITY ? 0.f : -m_ref * cm;       // (a row that sees nothing yet: every exponential is 0)
-          float l0 = 0.f, l1 = 0.f, l2 = 0.f, l3 = 0.f;
-#pragma unroll
-          for (int hf = 0; hf < 2; ++hf) {
-            uint32_t *d = s + (FP8 ? 0 : hf * 64);
-            if constexpr (FP8) load_half(hf, d);
-            uint32_t packed[32];
-#pragma unroll
-            for (int i = 0; i < 64; i += 4) {
-              float p0 = tt_exp2(fmaf(__uint_as_float(d[i]), c, neg_mc)), p1 = tt_exp2(fmaf(__uint_as_float(d[i + 1]), c, neg_mc));
-              float p2 = tt_exp2(fmaf(__uint_as_float(d[i + 2]), c, neg_mc)), p3 = tt_exp2(fmaf(__uint_as_float(d[i + 3]), c, neg_mc));
-              l0 += p0; l1 += p1; l2 += p2; l3 += p3;
-              if constexpr (FP8) {
-                const float4 v4 = *reinterpret_cast<const float4 *>(vsc + hf * 64 + i);
+              for (int i = 0; i < 32; i += 4) {
+                float p0 = tt_exp2(fmaf(__uint_as_float(d[i]), c, neg_mc)), p1 = tt_exp2(fmaf(__uint_as_float(d[i + 1]), c, neg_mc));
+                float p2 = tt_exp2(fmaf(__uint_as_float(d[i + 2]), c, neg_mc)), p3 = tt_exp2(fmaf(__uint_as_float(d[i + 3]), c, neg_mc));
+                l0 += p0; l1 += p1; l2 += p2; l3 += p3;
+                const float4 v4 = vsc[ch * 8 + i / 4];
                 p0 *= v4.x; p1 *= v4.y; p2 *= v4.z; p3 *= v4.w;
-                if (edge) {                                                  // (the scale of an unseen row may be anything)
-                  const uint32_t wd = words[hf * 2 + (i >> 5)] >> (i & 31);
-                  p0 = (wd & 1u) ? p0 : 0.f; p1 = (wd & 2u) ? p1 : 0.f; p2 = (wd & 4u) ? p2 : 0.f; p3 = (wd & 8u) ? p3 : 0.f;
+                if (seen != 0xffffffffu) {                                    // (the scale of an unseen row may be anything)
+                  p0 = (seen >> i) & 1u ? p0 : 0.f; p1 = (seen >> i) & 2u ? p1 : 0.f; p2 = (seen >> i) & 4u ? p2 : 0.f; p3 = (seen >> i) & 8u ? p3 : 0.f;
                 }
-              }
-              if constexpr (FP8) {                                           // (an infinite scale stays infinite)
-                const __half2 h0 = __floats2half2_rn(p0, p1), h1 = __floats2half2_rn(p2, p3);
+                const __half2 h0 = __floats2half2_rn(p0, p1), h1 = __floats2half2_rn(p2, p3);      // (an infinite scale stays infinite)
                 packed[i / 2] = *reinterpret_cast<const uint32_t *>(&h0);
                 packed[i / 2 + 1] = *reinterpret_cast<const uint32_t *>(&h1);
-              } else {
-                packed[i / 2] = F16 ? tc::pack_f16x2(p0, p1) : tc::pack_bf16x2(p0, p1);
-                packed[i / 2 + 1] = F16 ? tc::pack_f16x2(p2, p3) : tc::pack_bf16x2(p2, p3);
               }
+              tc::tmem_st_32x32b_x16(t_s + (ch >> 1) * 64 + (ch & 1) * 16, packed);      // (chunk 3 is still to be read when chunk 2 is overwritten)
+              if (ch & 1) announce(ch >> 1);
             }
-            tc::tmem_st_32x32b_x32(t_s + hf * 32, packed);      // over scores that have been read for the last time
-            tc::tmem_st_wait();
-            tc::tc_fence_before_sync();
-            __syncwarp();
-            if (lane == 0) tc::mbar_arrive(tc::smem_u32(hf ? &p_ready[w] : &p_half[w]));
+            l += (l0 + l1) + (l2 + l3);
           }
-          l += (l0 + l1) + (l2 + l3);
-          first = false;
         } else {
+          if (!FP8 && !(ok = wait(&s_full[w], sc & 1))) break;
           tc::tc_fence_before_sync();
           __syncwarp();
           if (lane == 0) {
-            tc::mbar_arrive(tc::smem_u32(&p_half[w]));
-            tc::mbar_arrive(tc::smem_u32(&p_ready[w]));
+            tc::mbar_arrive(tc::smem_u32(&p_part[w]));
+            tc::mbar_arrive(tc::smem_u32(&p_part[2 + w]));
           }
         }
+        ++sc;
       }
       if (!ok) break;
       // ---- the piece's result.  Both streams meet here once (W = 1: to join their halves of the keys).
@@ -883,7 +923,7 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
     } while (it.next(a));
   } else if constexpr (FP8) {
     // -------------------------------------------------------------------- widening warps: codes -> swizzled halves, scales; queries
-    const int t = threadIdx.x - 11 * 32;
+    const int t = threadIdx.x - 10 * 32;
     int cc = 0, tile = 0, item = 0;
     bool ok = true;
     do {
@@ -940,7 +980,7 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
 #pragma unroll
         for (int kv = 0; kv < 2; ++kv, ++cc) {
           const int cs = cc % L::CS, ds = kv ? tile % L::VS : 0;
-          const uint8_t *src = smem + L::C + cs * L::CODE_TILE;
+          const uint4 *src = reinterpret_cast<const uint4 *>(smem + L::C + cs * L::CODE_TILE) + t;
           uint8_t *dst = smem + (kv ? L::V : L::K) + ds * L::TILE;
           ok = ok && wait(&c_full[cs], (cc / L::CS) & 1) && (kv ? wait(&v_empty[ds], ((tile / L::VS) & 1) ^ 1) : wait(&k_empty[0], (tile & 1) ^ 1));
           if (!ok) break;
@@ -956,15 +996,17 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
           const int rr0 = t / PER_ROW, col = t % PER_ROW * 16, u = (col & 63) >> 3;
           uint8_t *line = dst + (col >> 6) * L::CHUNK + rr0 * 128;
           uint4 *y0 = reinterpret_cast<uint4 *>(line + ((u ^ (rr0 & 7)) << 4)), *y1 = reinterpret_cast<uint4 *>(line + (((u + 1) ^ (rr0 & 7)) << 4));
-          const uint4 *x = reinterpret_cast<const uint4 *>(src) + t;
+          uint4 c4[PER_ROW];
+#pragma unroll
+          for (int i = 0; i < PER_ROW; ++i) c4[i] = src[i * 128];
 #pragma unroll
           for (int i = 0; i < PER_ROW; ++i) {
-            uint4 c4 = x[i * 128], h0, h1;
-            if (rr0 + i * STEP >= live) c4 = make_uint4(0u, 0u, 0u, 0u);
-            widen4(c4.x, h0.x, h0.y);
-            widen4(c4.y, h0.z, h0.w);
-            widen4(c4.z, h1.x, h1.y);
-            widen4(c4.w, h1.z, h1.w);
+            uint4 h0, h1;
+            if (rr0 + i * STEP >= live) c4[i] = make_uint4(0u, 0u, 0u, 0u);
+            widen4(c4[i].x, h0.x, h0.y);
+            widen4(c4[i].y, h0.z, h0.w);
+            widen4(c4[i].z, h1.x, h1.y);
+            widen4(c4[i].w, h1.z, h1.w);
             y0[i * STEP * 8] = h0;
             y1[i * STEP * 8] = h1;
           }
