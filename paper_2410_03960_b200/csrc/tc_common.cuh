@@ -268,6 +268,11 @@ __device__ __forceinline__ F2 add2(F2 a, F2 b) {
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.u) : "l"(a.u), "l"(b.u));
   return r;
 }
+__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
+  F2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.u) : "l"(a.u), "l"(b.u));
+  return r;
+}
 __device__ __forceinline__ float max_nan(float a, float b) {      // NaN if either is
   float r;
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
@@ -300,10 +305,10 @@ __device__ __forceinline__ uint32_t pack_act(float lo, float hi, bool f16) {
 
 // ---- host: tensor maps ---------------------------------------------------------------------------------------
 // Row-major bf16 matrix [rows, cols] (row stride ld elements); box = box_cols x box_rows, 128-byte swizzle
-// (box_cols must be 64), out-of-range rows/cols read as zero; swizzle false: the box's rows packed as they are.
-// Returns 0 on success.
+// (box_cols must be 64; 64-byte swizzle: 32), out-of-range rows/cols read as zero.  Returns 0 on success.
+enum TmapSwizzle : int { TMAP_SWIZZLE_128B, TMAP_SWIZZLE_64B };
 int make_tmap_2d_bf16(CUtensorMap *out, const void *base, uint64_t rows, uint64_t cols, uint64_t ld,
-                      uint32_t box_rows, uint32_t box_cols, bool swizzle = true);
+                      uint32_t box_rows, uint32_t box_cols, TmapSwizzle swizzle = TMAP_SWIZZLE_128B);
 // bf16 tensor [d2][d1][d0] with element strides (s2, s1, 1); box (b0, b1, b2), 128-byte swizzle.
 int make_tmap_3d_bf16(CUtensorMap *out, const void *base, uint64_t d0, uint64_t d1, uint64_t d2, uint64_t s1,
                       uint64_t s2, uint32_t b0, uint32_t b1, uint32_t b2);

@@ -320,24 +320,27 @@ def run_tree(c, **kw):
 
 def check_tree(c, out, lse, scale=None):
     """|out - o| <= u |o| + (u_P + e) A with A = sum p |v|: u_P the rounding of the probabilities to 16 bits (the 16-bit paths; with an
-    FP8 cache they carry the rows' scale and are bf16), e the relative error of a probability: twice that of its exponent, which is the
+    FP8 cache they carry the rows' scale and are halves: 2^-11 relative, or -- steps of 2^-24 below 2^-14, with a reference that keeps the
+    row's largest P at 1 or more -- 2^-25 of that largest: 2^-25 G, the G of verify_reference), e the relative error of a probability: twice that of its exponent, which is the
     products' (hd + 2) 2^-24 of sum |q k| scale, plus 2^-20 for exp2 and the fp32 sums over the keys (pairwise inside a tile, then a
     chain over tiles and splits)."""
     u = u_of(c["dt"])
     if c["fp8"]:
         k, v = e4m3(c["k"]) * f64(c["ks"])[:, None, None], e4m3(c["v"]) * f64(c["vs"])[:, None, None]
-        u_p = 2.0 ** -8 if c["dt"] != FF else 0.0
+        u_p = 2.0 ** -11 if c["dt"] != FF else 0.0
+        extra = dict(v_scale=f64(c["vs"]), v_codes=e4m3(c["v"]))
     else:
         k, v = f64(c["k"]), f64(c["v"])
         u_p = u if c["dt"] != FF else 0.0
-    want, wl, A, Z = R.tree_attention(f64(c["q"]), k, v, c["past"], c["cu"], c["rows"], c["sees"], scale)
+        extra = {}
+    want, wl, A, Z, G = R.tree_attention(f64(c["q"]), k, v, c["past"], c["cu"], c["rows"], c["sees"], scale, **extra)
     dz = (c["hd"] + 2) * 2.0 ** -24 * Z + 2.0 ** -20 + 2.0 ** -24 * np.where(np.isfinite(wl), np.abs(wl), 0) * 4
     keys = c["max_kv"] / 128 + 64
     e = (2 * dz + keys * 2.0 ** -24)[..., None]
     got, gl = f64(out), f64(lse)
     sees = np.isfinite(wl)
     assert np.array_equal(sees, np.isfinite(gl)) and (gl[~sees] == -np.inf).all() and (got[~sees] == 0).all()
-    bad = np.abs(got - want) > u * np.abs(want) + (u_p * 1.01 + e) * A + tiny_of(c["dt"])
+    bad = np.abs(got - want) > u * np.abs(want) + (u_p * 1.01 + e) * A + (2.0 ** -25 * G if c["dt"] != FF else 0.0) + tiny_of(c["dt"])
     assert not bad.any(), (np.argwhere(bad)[:4], np.abs(got - want).max())
     assert (np.abs(gl - wl)[sees] <= (dz + keys * 2.0 ** -24 + 2.0 ** -22 * (1 + np.abs(np.where(sees, wl, 0))))[sees]).all()
 
@@ -459,6 +462,21 @@ def test_tree_attention_large_scores(kind):
             c["k"][neg] = 0xB8
         else:
             c["k"][rows] = ramp[:, None, None].to(c["dt"]).expand(-1, 2, 128)
+        check_tree(c, *run_tree(c))
+
+
+@pytest.mark.parametrize("n", [1, 10, 20, 40])
+def test_tree_attention_every_fp8_code(n):
+    """All 254 numbers of e4m3, subnormal ones and zeros of both signs among them, in K and V; 4 to 160 rows per KV head (a tile of few
+    rows is laid out several times); row scales over many powers of two."""
+    for dt in (BF, HF, FF):
+        c = tree_case(33, [(700, n), (3, n)], 8, 2, 128, dt, fp8=True)
+        numbers = torch.tensor([i for i in range(256) if i & 0x7F != 0x7F], dtype=torch.uint8, device="cuda")
+        g = torch.Generator(device="cuda").manual_seed(5)
+        for t in (c["k"], c["v"]):
+            t.copy_(numbers[torch.randint(0, 254, t.shape, generator=g, device="cuda")])
+        c["ks"] = torch.exp2(torch.randint(-14, -8, c["ks"].shape, generator=g, device="cuda").float()) * 1.37
+        c["vs"] = torch.exp2(torch.randint(-30, 3, c["vs"].shape, generator=g, device="cuda").float()) * 1.19
         check_tree(c, *run_tree(c))
 
 

@@ -57,15 +57,16 @@ def norm_rope_bwd(x, dy, gain, eps, positions, theta):
     return r * (dh - xh * (dh * xh).mean(-1, keepdims=True)), (dz * xh).sum((0, 1))
 
 
-def tree_attention(q, k, v, past, cu, rows, sees, scale=None):
+def tree_attention(q, k, v, past, cu, rows, sees, scale=None, v_scale=None, v_codes=None):
     """q [T, n_q, hd]; k, v [cache rows, n_kv, hd] (values); rows[b]: cache row of every key of sequence b (-1: reads as zeros); sees[b]:
     bool [new, new].  -> out, lse, A (sum p |v|, what a relative error of the probabilities is multiplied with), Z (the largest
-    sum |q k| scale of a row, what a relative error of the products is multiplied with)."""
+    sum |q k| scale of a row, what a relative error of the products is multiplied with), and with v_scale / v_codes (v being their product)
+    G = max_j(p_j scale_j) sum_j |code_j|, what an error relative to a row's largest scale-weighted probability is multiplied with."""
     T, n_q, hd = q.shape
     rep = n_q // k.shape[1]
     scale = 1.0 / math.sqrt(hd) if scale is None else scale
     out, lse = np.zeros((T, n_q, hd)), np.full((T, n_q), -np.inf)
-    A, Z = np.zeros((T, n_q, hd)), np.zeros((T, n_q))
+    A, Z, G = np.zeros((T, n_q, hd)), np.zeros((T, n_q)), np.zeros((T, n_q, hd))
     for b in range(len(past)):
         n = cu[b + 1] - cu[b]
         if n == 0:
@@ -86,7 +87,10 @@ def tree_attention(q, k, v, past, cu, rows, sees, scale=None):
                 A[cu[b] + i, h] = p @ np.abs(vv[:, h // rep]) / p.sum()
                 Z[cu[b] + i, h] = (np.abs(kk[:, h // rep]) @ np.abs(x)).max() * scale
                 lse[cu[b] + i, h] = m + np.log(p.sum())
-    return out, lse, A, Z
+                if v_scale is not None:
+                    seen = np.maximum(r, 0)[vis[i]]
+                    G[cu[b] + i, h] = (p * v_scale[seen]).max() / p.sum() * np.abs(v_codes[seen, h // rep]).sum(0)
+    return out, lse, A, Z, G
 
 
 def token_logprobs(x, targets, temperature, top_k):
