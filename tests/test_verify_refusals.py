@@ -124,3 +124,21 @@ def test_wrappers_refuse_host_tensors(lib):
                  lambda: P.tree_attention(h, h, h, i, i, 1, 1, row0=i)):
         with pytest.raises(ValueError):
             call()
+
+
+def test_wrappers_refuse_what_is_no_tensor(lib):
+    import paper_2410_03960_b200 as P
+    with pytest.raises(ValueError):
+        P.token_logprobs_bwd("logits", None, None, None, None)
+    with pytest.raises(ValueError):
+        P.tree_attention(None, None, None, None, None, 1, 1)
+
+
+def test_the_extension_checks_its_own_arguments(lib):
+    from paper_2410_03960_b200 import verify
+    ext = verify._load()
+    for name in ("plan_pages", "qk_norm_rope", "qk_norm_rope_bwd", "tree_attention", "token_logprobs", "token_logprobs_bwd", "bind"):
+        with pytest.raises(TypeError):
+            getattr(ext, name)()
+    with pytest.raises(ValueError):
+        ext.bind(RuntimeError, {})
