@@ -10,9 +10,11 @@
 // (scale = max(max|y|, 2^-64) / 448, code = e4m3(y / scale), as swiftkv_quantize_rows_fp8), not from a 16-bit copy of it.
 //
 // What bounds it: HBM, every row read once and written once.  Vector form: hd/16 lanes hold one head, 16 bytes of its lower
-// and 16 bytes of its upper half each, so a rotation pair sits in one thread, a head's mean needs log2(hd/16) shuffles, and
-// a thread's cos / sin / gain values serve every head that it walks over.  Other shapes, fp32 and unaligned tensors take the
-// general form (one warp per head, a pair per lane and step).
+// and 16 bytes of its upper half each, so a rotation pair sits in one thread and a head's mean needs log2(hd/16) shuffles; as
+// many blocks as run at once walk over the (token, head) pairs, and what limits them is how many warps' registers fit beside
+// the loads under way.  Other shapes, fp32 and unaligned tensors take the general form (one warp per head, a pair per lane
+// and step).  Measured, 32 + 8 heads of 128, bf16: 16411 tokens 73 us (5.5 TB/s; torch's copy of as many bytes 64 us), 4096
+// tokens into an FP8 cache 27 us; gradient of 8195 tokens 55 us (4.7 TB/s).
 #include "common.cuh"
 #include "tc_common.cuh"
 
@@ -73,19 +75,18 @@ __device__ __forceinline__ uint8_t code_of(float x, float scale) {
 }
 __device__ __forceinline__ float row_scale(float amax) { return __fdiv_rn(fmaxf(amax, FP8_AMAX_FLOOR), FP8_MAX); }
 
-__device__ __forceinline__ int checked_position(const RopeArgs &a, int t) {
-  const int p = a.positions[t];
-  if (p >= 0 && p < a.max_pos) return p;
-  if (threadIdx.x == 0) atomicOr(a.status, STATUS_BAD_TOKEN);
-  return p < 0 ? 0 : a.max_pos - 1;
+__device__ __forceinline__ int checked_position(int p, int max_pos, unsigned int *status, bool reports) {
+  if (p >= 0 && p < max_pos) return p;
+  if (reports) atomicOr(status, STATUS_BAD_TOKEN);
+  return p < 0 ? 0 : max_pos - 1;
 }
-// cache row of token t, -1: not stored
-__device__ __forceinline__ int checked_slot(const RopeArgs &a, int t) {
-  const int s = a.slot_map ? a.slot_map[t] : t;
+// cache row of a token whose slot is s, -1: not stored
+__device__ __forceinline__ int checked_slot(const RopeArgs &a, int s, bool reports) {
   if (s < a.cache_rows) return s < 0 ? -1 : s;
-  if (threadIdx.x == 0) atomicOr(a.status, STATUS_BAD_TOKEN);
+  if (reports) atomicOr(a.status, STATUS_BAD_TOKEN);
   return -1;
 }
+__device__ __forceinline__ int slot_of(const RopeArgs &a, int t) { return a.slot_map ? a.slot_map[t] : t; }
 
 __device__ __forceinline__ float block_max_all(float v, float *red, int warps) {
   v = warp_max(v);
@@ -96,91 +97,204 @@ __device__ __forceinline__ float block_max_all(float v, float *red, int warps) {
   return m;
 }
 
-__device__ __forceinline__ void load8f(const float *p, float (&x)[8]) {
+// ---- two fp32 values per operation; eight of them from 16 bytes of a 16-bit type ---------------------------------------
+using tc::F2;
+using tc::add2;
+using tc::fma2;
+using tc::mul2;
+__device__ __forceinline__ F2 both(float v) { return F2{{v, v}}; }
+template <typename T>
+__device__ __forceinline__ void unpack(const uint4 &v, F2 (&x)[4]) {
+  float f[8];
+  unpack8(v, f, (const T *)nullptr);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = F2{{f[2 * i], f[2 * i + 1]}};
+}
+template <typename T>
+__device__ __forceinline__ uint4 pack(const F2 (&x)[4]) {
+  const float f[8] = {x[0].f[0], x[0].f[1], x[1].f[0], x[1].f[1], x[2].f[0], x[2].f[1], x[3].f[0], x[3].f[1]};
+  return pack8(f, (const T *)nullptr);
+}
+__device__ __forceinline__ void load8(const float *p, F2 (&x)[4]) {
   const float4 a = __ldg(reinterpret_cast<const float4 *>(p)), b = __ldg(reinterpret_cast<const float4 *>(p) + 1);
-  x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+  x[0] = F2{{a.x, a.y}}; x[1] = F2{{a.z, a.w}}; x[2] = F2{{b.x, b.y}}; x[3] = F2{{b.z, b.w}};
+}
+template <int L>
+__device__ __forceinline__ float sum_lanes(float v) {
+#pragma unroll
+  for (int o = L / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+__device__ __forceinline__ uint2 codes8(const F2 (&x)[4], float scale) {
+  uint32_t w[2] = {0u, 0u};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) w[i / 4] |= (uint32_t)code_of(x[i / 2].f[i & 1], scale) << (8 * (i & 3));
+  return make_uint2(w[0], w[1]);
+}
+// (token, head) pairs in order, `groups` of them per step of a block and `blocks` blocks side by side
+struct Walk {
+  int steps, groups, heads, t_step, h_step;                 // steps of this block: the same for all its threads
+  long long first;
+  __device__ __forceinline__ Walk(long long pairs, int block, int blocks, int groups_, int heads_) : groups(groups_), heads(heads_) {
+    const long long step = (long long)blocks * groups;
+    first = (long long)block * groups;
+    steps = first < pairs ? (int)((pairs - first + step - 1) / step) : 0;
+    t_step = (int)(step / heads);
+    h_step = (int)(step % heads);
+  }
+  __device__ __forceinline__ void start(int group, int &t, int &h) const {
+    t = (int)((first + group) / heads);
+    h = (int)((first + group) % heads);
+  }
+  __device__ __forceinline__ void advance(int &t, int &h) const {
+    t += t_step;
+    h += h_step;
+    if (h >= heads) { h -= heads; ++t; }
+  }
+};
+
+// a head's 16 values of this thread -> normed (norm; g: gains of the lower / upper half) and rotated (plain: left as they are)
+template <int L>
+__device__ __forceinline__ void norm_rotate(F2 (&lo)[4], F2 (&hi)[4], bool norm, bool plain, const F2 (&gl)[4], const F2 (&gh)[4], const F2 (&c)[4],
+                                            const F2 (&s)[4], float eps) {
+  float r = 1.f;
+  if (norm) {
+    F2 ss = mul2(lo[0], lo[0]);
+#pragma unroll
+    for (int i = 1; i < 4; ++i) ss = fma2(lo[i], lo[i], ss);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) ss = fma2(hi[i], hi[i], ss);
+    r = rsqrtf(sum_lanes<L>(ss.f[0] + ss.f[1]) * (1.f / (16 * L)) + eps);
+  }
+  if (plain) return;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    F2 a = lo[i], b = hi[i];
+    if (norm) { a = mul2(mul2(a, gl[i]), both(r)); b = mul2(mul2(b, gh[i]), both(r)); }
+    const F2 bs = mul2(b, s[i]), as = mul2(a, s[i]);
+    lo[i] = fma2(a, c[i], F2{{-bs.f[0], -bs.f[1]}});
+    hi[i] = fma2(b, c[i], as);
+  }
 }
 
-// ---- forward, vector form: block (token) or, FP8, (token, Q / K / V) --------------------------------------
-// UNITS heads are loaded together per thread, so that their loads are in flight at once
-template <typename T, int L, int UNITS>
-__global__ void qk_norm_rope_vec_kernel(RopeArgs a) {
-  const int t = blockIdx.x, half = 8 * L;
-  const int sub = threadIdx.x % L, unit0 = threadIdx.x / L, step = blockDim.x / L;
-  const int n_units = a.n_q + 2 * a.n_kv;
-  const int slot = checked_slot(a, t), pos = checked_position(a, t);
-  uint4 lo[UNITS], hi[UNITS];
-  auto source = [&](int u) -> const T * {
-    if (u < a.n_q) return reinterpret_cast<const T *>(a.q) + (size_t)t * a.q_stride + (size_t)u * (2 * half);
-    u -= a.n_q;
-    if (u < a.n_kv) return reinterpret_cast<const T *>(a.k) + (size_t)t * a.k_stride + (size_t)u * (2 * half);
-    return reinterpret_cast<const T *>(a.v) + (size_t)t * a.v_stride + (size_t)(u - a.n_kv) * (2 * half);
-  };
-  float c[8], s[8];
-  for (int base = 0; base < n_units; base += step * UNITS) {
+// ---- forward, vector form: L lanes per head -----------------------------------------------------------------------------
+// Threads of a block and blocks per SM: registers for one step of loads under way beside one at work, without a spill (16411 tokens
+// of the 8B shape: 73 us; 3 x 256 threads 76, 2 x 256 89, 4 x 256 with a few spilled 79, gains read again from L1 82).  FP8 rows
+// take larger blocks: a row's maximum is taken over one block.
+__host__ __device__ constexpr int rv_threads(bool fp8) { return fp8 ? 256 : 128; }
+__host__ __device__ constexpr int rv_blocks_per_sm(bool fp8) { return fp8 ? 3 : 7; }
+// The first q_blocks blocks walk over the (token, query head) pairs, the next k_blocks over the key heads, the rest over the value
+// heads, as many blocks as run at once and the next pair's loads under way while one is computed.
+// FP8: the rest are rows of keys and values, RV_THREADS / row_lanes of them a block, a row's heads side by side in registers.
+template <typename T, int L, bool FP8>
+__global__ void __launch_bounds__(rv_threads(FP8), rv_blocks_per_sm(FP8)) qk_norm_rope_vec_kernel(RopeArgs a, int q_blocks, int k_blocks, int row_lanes) {
+  constexpr int RV_THREADS = rv_threads(FP8);
+  constexpr int half = 8 * L, HD = 16 * L, GROUPS = RV_THREADS / L;
+  const int sub = threadIdx.x % L, unit0 = threadIdx.x / L;
+  if (FP8 && (int)blockIdx.x >= q_blocks) {
+    __shared__ float red[RV_THREADS / 32];
+    const int lane = threadIdx.x % row_lanes, h = lane / L;
+    const long long row = (long long)(blockIdx.x - q_blocks) * (RV_THREADS / row_lanes) + threadIdx.x / row_lanes;
+    const int t = (int)(row >> 1);
+    const bool is_v = row & 1, have = t < a.tokens && h < a.n_kv;
+    F2 x[4], y[4];
+    int slot = -1;
 #pragma unroll
-    for (int i = 0; i < UNITS; ++i) {
-      const int u = base + unit0 + i * step;
-      if (u < n_units) {
-        const uint4 *p = reinterpret_cast<const uint4 *>(source(u) + 8 * sub);
-        lo[i] = __ldcs(p);
-        hi[i] = __ldcs(p + L);
-      }
-    }
-    if (base == 0) {
-      load8f(a.cos_tab + (size_t)pos * half + 8 * sub, c);
-      load8f(a.sin_tab + (size_t)pos * half + 8 * sub, s);
-    }
+    for (int i = 0; i < 4; ++i) x[i] = y[i] = both(0.f);
+    F2 c[4], s[4], gl[4], gh[4];
+    const T *gain = reinterpret_cast<const T *>(is_v ? nullptr : a.k_gain);
 #pragma unroll
-    for (int i = 0; i < UNITS; ++i) {
-      const int u = base + unit0 + i * step;
-      const bool ok = u < n_units, is_q = u < a.n_q, is_v = u >= a.n_q + a.n_kv;
-      // every lane of a warp walks the shuffles of the norm (heads of one warp may belong to q, K and V)
-      float x0[8], x1[8];
-      if (!ok) { lo[i] = hi[i] = make_uint4(0u, 0u, 0u, 0u); }
-      unpack8(lo[i], x0, (const T *)nullptr);
-      unpack8(hi[i], x1, (const T *)nullptr);
-      const T *gain = reinterpret_cast<const T *>(is_q ? a.q_gain : a.k_gain);
-      float r = 1.f;
-      if (a.q_gain || a.k_gain) {
-        float ss = 0.f;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) ss = fmaf(x0[j], x0[j], fmaf(x1[j], x1[j], ss));
-#pragma unroll
-        for (int o = L / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-        r = rsqrtf(ss * (1.f / (16 * L)) + a.eps);
-      }
-      if (!ok) continue;
-      if (is_v) {
-        if (slot >= 0) {
-          uint4 *d = reinterpret_cast<uint4 *>(reinterpret_cast<T *>(a.v_out) + ((size_t)slot * a.n_kv + (u - a.n_q - a.n_kv)) * (2 * half) + 8 * sub);
-          d[0] = lo[i];
-          d[L] = hi[i];
+    for (int i = 0; i < 4; ++i) { c[i] = gl[i] = gh[i] = both(1.f); s[i] = both(0.f); }
+    if (have) {
+      const T *src = is_v ? reinterpret_cast<const T *>(a.v) + (size_t)t * a.v_stride : reinterpret_cast<const T *>(a.k) + (size_t)t * a.k_stride;
+      const uint4 *p = reinterpret_cast<const uint4 *>(src + (size_t)h * HD + 8 * sub);
+      const uint4 lo = __ldcs(p), hi = __ldcs(p + L);
+      const int pos = checked_position(a.positions[t], a.max_pos, a.status, lane == 0);
+      slot = checked_slot(a, slot_of(a, t), lane == 0);
+      if (!is_v) {
+        load8(a.cos_tab + (size_t)pos * half + 8 * sub, c);
+        load8(a.sin_tab + (size_t)pos * half + 8 * sub, s);
+        if (gain) {
+          unpack<T>(__ldg(reinterpret_cast<const uint4 *>(gain + 8 * sub)), gl);
+          unpack<T>(__ldg(reinterpret_cast<const uint4 *>(gain + half + 8 * sub)), gh);
         }
-        continue;
       }
-      if (gain) {
-        float g[8];
-        unpack8(__ldg(reinterpret_cast<const uint4 *>(gain + 8 * sub)), g, (const T *)nullptr);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x0[j] *= r * g[j];
-        unpack8(__ldg(reinterpret_cast<const uint4 *>(gain + half + 8 * sub)), g, (const T *)nullptr);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x1[j] *= r * g[j];
-      }
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float y0 = x0[j] * c[j] - x1[j] * s[j], y1 = x1[j] * c[j] + x0[j] * s[j];
-        x0[j] = y0;
-        x1[j] = y1;
-      }
-      uint4 *d;
-      if (is_q) d = reinterpret_cast<uint4 *>(reinterpret_cast<T *>(a.q_out) + (size_t)t * a.qo_stride + (size_t)u * (2 * half) + 8 * sub);
-      else if (slot >= 0) d = reinterpret_cast<uint4 *>(reinterpret_cast<T *>(a.k_out) + ((size_t)slot * a.n_kv + (u - a.n_q)) * (2 * half) + 8 * sub);
-      else continue;
-      d[0] = pack8(x0, (const T *)nullptr);
-      d[L] = pack8(x1, (const T *)nullptr);
+      unpack<T>(lo, x);
+      unpack<T>(hi, y);
     }
+    norm_rotate<L>(x, y, gain != nullptr, is_v, gl, gh, c, s, a.eps);       // (every lane walks its shuffles)
+    float amax = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) amax = fmaxf(fmaxf(fmaxf(fabsf(x[i].f[0]), fabsf(x[i].f[1])), fmaxf(fabsf(y[i].f[0]), fabsf(y[i].f[1]))), amax);
+    for (int o = (row_lanes < 32 ? row_lanes : 32) / 2; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+    if (row_lanes > 32) {
+      if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = amax;
+      __syncthreads();
+      for (int w = 0; w < row_lanes / 32; ++w) amax = fmaxf(amax, red[threadIdx.x / row_lanes * (row_lanes / 32) + w]);
+    }
+    if (slot < 0) return;
+    const float scale = row_scale(amax);
+    if (lane == 0) (is_v ? a.v_scale : a.k_scale)[slot] = scale;
+    uint8_t *d = reinterpret_cast<uint8_t *>(is_v ? a.v_out : a.k_out) + ((size_t)slot * a.n_kv + h) * HD + 8 * sub;
+    *reinterpret_cast<uint2 *>(d) = codes8(x, scale);
+    *reinterpret_cast<uint2 *>(d + half) = codes8(y, scale);
+    return;
+  }
+  const int role = (int)blockIdx.x < q_blocks ? ROLE_Q : (int)blockIdx.x < q_blocks + k_blocks ? ROLE_K : ROLE_V;
+  const int first = role == ROLE_Q ? 0 : role == ROLE_K ? q_blocks : q_blocks + k_blocks;
+  const int blocks = role == ROLE_Q ? q_blocks : role == ROLE_K ? k_blocks : (int)gridDim.x - first;
+  const int heads = role == ROLE_Q ? a.n_q : a.n_kv;
+  const T *src = reinterpret_cast<const T *>(role == ROLE_Q ? a.q : role == ROLE_K ? a.k : a.v);
+  const long long stride = role == ROLE_Q ? a.q_stride : role == ROLE_K ? a.k_stride : a.v_stride;
+  const long long out_stride = role == ROLE_Q ? a.qo_stride : (long long)a.n_kv * HD;
+  T *dst = reinterpret_cast<T *>(role == ROLE_Q ? a.q_out : role == ROLE_K ? a.k_out : a.v_out);
+  const T *gain = reinterpret_cast<const T *>(role == ROLE_Q ? a.q_gain : role == ROLE_K ? a.k_gain : nullptr);
+  uint4 gain_lo = make_uint4(0u, 0u, 0u, 0u), gain_hi = gain_lo;
+  if (gain) {
+    gain_lo = __ldg(reinterpret_cast<const uint4 *>(gain + 8 * sub));
+    gain_hi = __ldg(reinterpret_cast<const uint4 *>(gain + half + 8 * sub));
+  }
+  const Walk walk((long long)a.tokens * heads, blockIdx.x - first, blocks, GROUPS, heads);
+  int t, h;
+  walk.start(unit0, t, h);
+  struct Unit { uint4 lo, hi; int pos, row; };               // row: of the output, -1 none
+  auto fetch = [&](Unit &n) {
+    n.lo = n.hi = make_uint4(0u, 0u, 0u, 0u);
+    n.pos = 0;
+    n.row = -1;
+    if (t >= a.tokens) return;
+    const uint4 *p = reinterpret_cast<const uint4 *>(src + (size_t)t * stride + h * HD + 8 * sub);
+    n.lo = __ldcs(p);
+    n.hi = __ldcs(p + L);
+    n.row = role == ROLE_Q ? t : slot_of(a, t);
+    if (role != ROLE_V) n.pos = a.positions[t];
+  };
+  Unit next;
+  fetch(next);
+  for (int left = walk.steps; left > 0; --left) {
+    const Unit now = next;
+    const int at = h * HD + 8 * sub;
+    walk.advance(t, h);
+    fetch(next);
+    const int row = role == ROLE_Q ? now.row : checked_slot(a, now.row, sub == 0);
+    uint4 lo = now.lo, hi = now.hi;
+    if (role != ROLE_V) {
+      const int pos = checked_position(now.pos, a.max_pos, a.status, sub == 0);
+      F2 c[4], s[4], x[4], y[4], gl[4], gh[4];
+      load8(a.cos_tab + (size_t)pos * half + 8 * sub, c);
+      load8(a.sin_tab + (size_t)pos * half + 8 * sub, s);
+      unpack<T>(lo, x);
+      unpack<T>(hi, y);
+      unpack<T>(gain_lo, gl);
+      unpack<T>(gain_hi, gh);
+      norm_rotate<L>(x, y, gain != nullptr, false, gl, gh, c, s, a.eps);
+      lo = pack<T>(x);
+      hi = pack<T>(y);
+    }
+    if (row < 0) continue;
+    uint4 *d = reinterpret_cast<uint4 *>(dst + (size_t)row * out_stride + at);
+    __stcs(d, lo);
+    __stcs(d + L, hi);
   }
 }
 
@@ -194,8 +308,8 @@ __global__ void __launch_bounds__(RG_THREADS) qk_norm_rope_kernel(RopeArgs a, in
   const int t = blockIdx.x, role = first_role + blockIdx.y, half = a.hd >> 1;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const bool fp8 = role != ROLE_Q && a.k_scale != nullptr;
-  const int pos = checked_position(a, t);
-  const int slot = role == ROLE_Q ? 0 : checked_slot(a, t);
+  const int pos = checked_position(a.positions[t], a.max_pos, a.status, threadIdx.x == 0);
+  const int slot = role == ROLE_Q ? 0 : checked_slot(a, slot_of(a, t), threadIdx.x == 0);
   const int heads = role == ROLE_Q ? a.n_q : a.n_kv;
   const T *src = role == ROLE_Q ? reinterpret_cast<const T *>(a.q) + (size_t)t * a.q_stride
                 : role == ROLE_K ? reinterpret_cast<const T *>(a.k) + (size_t)t * a.k_stride : reinterpret_cast<const T *>(a.v) + (size_t)t * a.v_stride;
@@ -255,218 +369,220 @@ struct RopeBwdArgs {
   const int32_t *positions;
   const float *cos_tab, *sin_tab;
   void *dq_in, *dk_in;                       // [T][n][hd] contiguous; dq_in == dq, dk_in == dk allowed
-  float *partial;                            // [blocks][2][hd] gain gradients of each block
+  float *partial;                            // [blocks][hd] gain gradients of each block
   int tokens, n_q, n_kv, hd, max_pos;
   float eps;
   unsigned int *status;
 };
 constexpr int RB_THREADS = 256;
-constexpr int RB_BLOCKS_PER_SM = 4;
-
-// vector form: L lanes per head; a block walks over tokens, a thread over heads of a token; gain gradients stay in registers
+constexpr int RB_BLOCKS_PER_SM = 2;      // as many of the vector form as run at once
+// vector form: L lanes per head; the first q_blocks blocks walk over the (token, query head) pairs, the rest over the key heads, the next
+// pair's loads under way while one is computed; gain gradients stay in registers.  These hold it to 16 warps per SM, of 285 instructions
+// a pair and step: 55 us for 8195 tokens of the 8B shape (half as many elements per thread and 24 warps 59, loads by asynchronous
+// copies and two to four steps ahead 59, four times as many blocks 69).
 template <typename T, int L>
-__global__ void __launch_bounds__(RB_THREADS) qk_norm_rope_bwd_vec_kernel(RopeBwdArgs a) {
+__global__ void __launch_bounds__(RB_THREADS, RB_BLOCKS_PER_SM) qk_norm_rope_bwd_vec_kernel(RopeBwdArgs a, int q_blocks) {
   constexpr int half = 8 * L, HD = 16 * L, GROUPS = RB_THREADS / L;
   __shared__ float red[RB_THREADS / 32][HD];
   const int sub = threadIdx.x % L, unit0 = threadIdx.x / L;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-#pragma unroll 1
-  for (int which = 0; which < 2; ++which) {
-    const int heads = which ? a.n_kv : a.n_q;
-    const T *gain = reinterpret_cast<const T *>(which ? a.k_gain : a.q_gain);
-    const T *x = reinterpret_cast<const T *>(which ? a.k : a.q);
-    const long long x_stride = which ? a.k_stride : a.q_stride;
-    const T *dy = reinterpret_cast<const T *>(which ? a.dk : a.dq);
-    T *dx = reinterpret_cast<T *>(which ? a.dk_in : a.dq_in);
-    float gl[8], gh[8], al[8], ah[8];
+  const int which = (int)blockIdx.x >= q_blocks, first = which ? q_blocks : 0;
+  const int heads = which ? a.n_kv : a.n_q;
+  const T *gain = reinterpret_cast<const T *>(which ? a.k_gain : a.q_gain);
+  const T *x = reinterpret_cast<const T *>(which ? a.k : a.q);
+  const long long x_stride = which ? a.k_stride : a.q_stride;
+  const T *dy = reinterpret_cast<const T *>(which ? a.dk : a.dq);
+  T *dx = reinterpret_cast<T *>(which ? a.dk_in : a.dq_in);
+  F2 al[4], ah[4];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) al[j] = ah[j] = 0.f;
+  for (int j = 0; j < 4; ++j) al[j] = ah[j] = both(0.f);
+  uint4 gain_lo = make_uint4(0u, 0u, 0u, 0u), gain_hi = gain_lo;
+  if (gain) {
+    gain_lo = __ldg(reinterpret_cast<const uint4 *>(gain + 8 * sub));
+    gain_hi = __ldg(reinterpret_cast<const uint4 *>(gain + half + 8 * sub));
+  }
+  const Walk walk((long long)a.tokens * heads, blockIdx.x - first, which ? gridDim.x - q_blocks : q_blocks, GROUPS, heads);
+  int t, h;                               // (whole warps stay together for the shuffles)
+  walk.start(unit0, t, h);
+  struct Unit { uint4 d0, d1, v0, v1; int pos; };
+  auto fetch = [&](Unit &n) {
+    n.d0 = n.d1 = n.v0 = n.v1 = make_uint4(0u, 0u, 0u, 0u);
+    n.pos = 0;
+    if (t >= a.tokens) return;
+    const uint4 *p = reinterpret_cast<const uint4 *>(dy + ((size_t)t * heads + h) * HD + 8 * sub);
+    n.d0 = __ldcs(p);
+    n.d1 = __ldcs(p + L);
     if (gain) {
-      unpack8(__ldg(reinterpret_cast<const uint4 *>(gain + 8 * sub)), gl, (const T *)nullptr);
-      unpack8(__ldg(reinterpret_cast<const uint4 *>(gain + half + 8 * sub)), gh, (const T *)nullptr);
+      const uint4 *xp = reinterpret_cast<const uint4 *>(x + (size_t)t * x_stride + h * HD + 8 * sub);
+      n.v0 = __ldcs(xp);
+      n.v1 = __ldcs(xp + L);
     }
-    // (token, head) pairs in order, GROUPS of them per step of the block; whole warps stay together for the shuffles
-    const long long n_units = (long long)a.tokens * heads, grid_step = (long long)gridDim.x * GROUPS;
-    for (long long base = (long long)blockIdx.x * GROUPS; base < n_units; base += grid_step) {
-      const long long u = base + unit0;
-      const bool ok = u < n_units;
-      const int t = ok ? (int)(u / heads) : 0, h = ok ? (int)(u - (long long)t * heads) : 0;
-      uint4 d0 = make_uint4(0u, 0u, 0u, 0u), d1 = d0, v0 = d0, v1 = d0;
-      float c[8], s[8];
-      if (ok) {
-        const uint4 *p = reinterpret_cast<const uint4 *>(dy + ((size_t)t * heads + h) * HD + 8 * sub);
-        d0 = p[0];
-        d1 = p[L];
-        if (gain) {
-          const uint4 *xp = reinterpret_cast<const uint4 *>(x + (size_t)t * x_stride + (size_t)h * HD + 8 * sub);
-          v0 = xp[0];
-          v1 = xp[L];
-        }
-      }
-      int pos = a.positions[t];
-      if (pos < 0 || pos >= a.max_pos) {
-        if (sub == 0) atomicOr(a.status, STATUS_BAD_TOKEN);
-        pos = pos < 0 ? 0 : a.max_pos - 1;
-      }
-      load8f(a.cos_tab + (size_t)pos * half + 8 * sub, c);
-      load8f(a.sin_tab + (size_t)pos * half + 8 * sub, s);
-      float z0[8], z1[8], x0[8], x1[8];
-      unpack8(d0, z0, (const T *)nullptr);
-      unpack8(d1, z1, (const T *)nullptr);
+    n.pos = a.positions[t];
+  };
+  Unit next;
+  fetch(next);
+  for (int left = walk.steps; left > 0; --left) {
+    const Unit now = next;
+    const bool ok = t < a.tokens;
+    uint4 *o = reinterpret_cast<uint4 *>(dx + ((size_t)t * heads + h) * HD + 8 * sub);
+    walk.advance(t, h);
+    fetch(next);
+    const int pos = checked_position(now.pos, a.max_pos, a.status, sub == 0);
+    F2 c[4], s[4], z0[4], z1[4];
+    load8(a.cos_tab + (size_t)pos * half + 8 * sub, c);
+    load8(a.sin_tab + (size_t)pos * half + 8 * sub, s);
+    unpack<T>(now.d0, z0);
+    unpack<T>(now.d1, z1);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float w0 = z0[j] * c[j] + z1[j] * s[j], w1 = z1[j] * c[j] - z0[j] * s[j];
-        z0[j] = w0;
-        z1[j] = w1;
+    for (int j = 0; j < 4; ++j) {
+      const F2 s1 = mul2(z1[j], s[j]), s0 = mul2(z0[j], s[j]);
+      z0[j] = fma2(z0[j], c[j], s1);
+      z1[j] = fma2(z1[j], c[j], F2{{-s0.f[0], -s0.f[1]}});
+    }
+    if (gain) {
+      F2 x0[4], x1[4], gl[4], gh[4], ss = both(0.f), dot = both(0.f);
+      unpack<T>(gain_lo, gl);
+      unpack<T>(gain_hi, gh);
+      unpack<T>(now.v0, x0);
+      unpack<T>(now.v1, x1);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        ss = fma2(x0[j], x0[j], ss);
+        ss = fma2(x1[j], x1[j], ss);
+        dot = fma2(mul2(z0[j], gl[j]), x0[j], dot);
+        dot = fma2(mul2(z1[j], gh[j]), x1[j], dot);
       }
-      if (gain) {
-        unpack8(v0, x0, (const T *)nullptr);
-        unpack8(v1, x1, (const T *)nullptr);
-        float ss = 0.f, dot = 0.f;
+      const float r = rsqrtf(sum_lanes<L>(ss.f[0] + ss.f[1]) * (1.f / HD) + a.eps);
+      const float m = -sum_lanes<L>(dot.f[0] + dot.f[1]) * r * r * (1.f / HD);          // -mean(dz g xh) r, to be multiplied by x
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          ss = fmaf(x0[j], x0[j], fmaf(x1[j], x1[j], ss));
-          dot = fmaf(z0[j] * gl[j], x0[j], fmaf(z1[j] * gh[j], x1[j], dot));
-        }
-#pragma unroll
-        for (int o = L / 2; o > 0; o >>= 1) {
-          ss += __shfl_xor_sync(0xffffffffu, ss, o);
-          dot += __shfl_xor_sync(0xffffffffu, dot, o);
-        }
-        const float r = rsqrtf(ss * (1.f / HD) + a.eps);
-        const float m = dot * r * r * (1.f / HD);          // mean(dz g xh) r, to be multiplied by x
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          if (ok) { al[j] = fmaf(z0[j], x0[j] * r, al[j]); ah[j] = fmaf(z1[j], x1[j] * r, ah[j]); }
-          z0[j] = r * fmaf(-x0[j], m, z0[j] * gl[j]);
-          z1[j] = r * fmaf(-x1[j], m, z1[j] * gh[j]);
-        }
-      }
-      if (ok) {
-        uint4 *o = reinterpret_cast<uint4 *>(dx + ((size_t)t * heads + h) * HD + 8 * sub);
-        o[0] = pack8(z0, (const T *)nullptr);
-        o[L] = pack8(z1, (const T *)nullptr);
+      for (int j = 0; j < 4; ++j) {
+        al[j] = fma2(z0[j], mul2(x0[j], both(r)), al[j]);              // (a pair that is not there adds zeros)
+        ah[j] = fma2(z1[j], mul2(x1[j], both(r)), ah[j]);
+        z0[j] = mul2(both(r), fma2(x0[j], both(m), mul2(z0[j], gl[j])));
+        z1[j] = mul2(both(r), fma2(x1[j], both(m), mul2(z1[j], gh[j])));
       }
     }
-    if (!gain) continue;
-    // lanes sub, sub + L, ... of a warp, then the warps, in a fixed order
+    if (ok) {
+      __stcs(o, pack<T>(z0));
+      __stcs(o + L, pack<T>(z1));
+    }
+  }
+  if (!gain) return;
+  // lanes sub, sub + L, ... of a warp, then the warps, in a fixed order
 #pragma unroll
-    for (int o = L; o < 32; o <<= 1)
+  for (int o = L; o < 32; o <<= 1)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        al[j] += __shfl_xor_sync(0xffffffffu, al[j], o);
-        ah[j] += __shfl_xor_sync(0xffffffffu, ah[j], o);
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        al[j].f[q] += __shfl_xor_sync(0xffffffffu, al[j].f[q], o);
+        ah[j].f[q] += __shfl_xor_sync(0xffffffffu, ah[j].f[q], o);
       }
-    __syncthreads();                 // (the previous tensor's sums have been read)
-    if (lane < L) {
+  if (lane < L) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) { red[warp][8 * sub + j] = al[j]; red[warp][half + 8 * sub + j] = ah[j]; }
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < HD; i += RB_THREADS) {
-      float v = 0.f;
+    for (int j = 0; j < 8; ++j) { red[warp][8 * sub + j] = al[j / 2].f[j & 1]; red[warp][half + 8 * sub + j] = ah[j / 2].f[j & 1]; }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < HD; i += RB_THREADS) {
+    float v = 0.f;
 #pragma unroll
-      for (int w = 0; w < RB_THREADS / 32; ++w) v += red[w][i];
-      a.partial[((size_t)blockIdx.x * 2 + which) * HD + i] = v;
-    }
+    for (int w = 0; w < RB_THREADS / 32; ++w) v += red[w][i];
+    a.partial[(size_t)blockIdx.x * HD + i] = v;
   }
 }
 
 // general form: one warp per head
 template <typename T>
-__global__ void __launch_bounds__(RB_THREADS) qk_norm_rope_bwd_kernel(RopeBwdArgs a) {
+__global__ void __launch_bounds__(RB_THREADS) qk_norm_rope_bwd_kernel(RopeBwdArgs a, int q_blocks) {
   extern __shared__ float rb_red[];            // [warps][hd]
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, half = a.hd >> 1;
   constexpr int WARPS = RB_THREADS / 32;
-  for (int which = 0; which < 2; ++which) {
-    const int heads = which ? a.n_kv : a.n_q;
-    const T *gain = reinterpret_cast<const T *>(which ? a.k_gain : a.q_gain);
-    const T *x = reinterpret_cast<const T *>(which ? a.k : a.q);
-    const long long x_stride = which ? a.k_stride : a.q_stride;
-    const T *dy = reinterpret_cast<const T *>(which ? a.dk : a.dq);
-    T *dx = reinterpret_cast<T *>(which ? a.dk_in : a.dq_in);
-    float a0[4] = {0.f, 0.f, 0.f, 0.f}, a1[4] = {0.f, 0.f, 0.f, 0.f};
-    const long long n_units = (long long)a.tokens * heads;
-    for (long long u = (long long)blockIdx.x * WARPS + warp; u < n_units; u += (long long)gridDim.x * WARPS) {
-      const int t = (int)(u / heads), h = (int)(u - (long long)t * heads);
-      int pos = a.positions[t];
-      if (pos < 0 || pos >= a.max_pos) {
-        if (lane == 0) atomicOr(a.status, STATUS_BAD_TOKEN);
-        pos = pos < 0 ? 0 : a.max_pos - 1;
-      }
-      const T *xr = x + (size_t)t * x_stride + (size_t)h * a.hd, *dr = dy + ((size_t)t * heads + h) * a.hd;
-      T *o = dx + ((size_t)t * heads + h) * a.hd;
-      float z0[4], z1[4], x0[4], x1[4], ss = 0.f, dot = 0.f;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int i = lane + 32 * j;
-        z0[j] = z1[j] = x0[j] = x1[j] = 0.f;
-        if (i < half) {
-          const float c = a.cos_tab[(size_t)pos * half + i], s = a.sin_tab[(size_t)pos * half + i];
-          const float d0 = to_f(dr[i]), d1 = to_f(dr[i + half]);
-          z0[j] = d0 * c + d1 * s;
-          z1[j] = d1 * c - d0 * s;
-          if (gain) {
-            x0[j] = to_f(xr[i]);
-            x1[j] = to_f(xr[i + half]);
-            ss = fmaf(x0[j], x0[j], fmaf(x1[j], x1[j], ss));
-            dot = fmaf(z0[j] * to_f(gain[i]), x0[j], fmaf(z1[j] * to_f(gain[i + half]), x1[j], dot));
-          }
-        }
-      }
-      float r = 1.f, m = 0.f;
-      if (gain) {
-        r = rsqrtf(warp_sum(ss) / a.hd + a.eps);
-        m = warp_sum(dot) * r * r / a.hd;
-      }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int i = lane + 32 * j;
-        if (i >= half) continue;
-        float y0 = z0[j], y1 = z1[j];
-        if (gain) {
-          a0[j] = fmaf(z0[j], x0[j] * r, a0[j]);
-          a1[j] = fmaf(z1[j], x1[j] * r, a1[j]);
-          y0 = r * fmaf(-x0[j], m, z0[j] * to_f(gain[i]));
-          y1 = r * fmaf(-x1[j], m, z1[j] * to_f(gain[i + half]));
-        }
-        o[i] = round_to<T>(y0);
-        o[i + half] = round_to<T>(y1);
-      }
-    }
-    if (!gain) continue;
-    __syncthreads();
+  const int which = (int)blockIdx.x >= q_blocks, first = which ? q_blocks : 0, blocks = which ? gridDim.x - q_blocks : q_blocks;
+  const int heads = which ? a.n_kv : a.n_q;
+  const T *gain = reinterpret_cast<const T *>(which ? a.k_gain : a.q_gain);
+  const T *x = reinterpret_cast<const T *>(which ? a.k : a.q);
+  const long long x_stride = which ? a.k_stride : a.q_stride;
+  const T *dy = reinterpret_cast<const T *>(which ? a.dk : a.dq);
+  T *dx = reinterpret_cast<T *>(which ? a.dk_in : a.dq_in);
+  float a0[4] = {0.f, 0.f, 0.f, 0.f}, a1[4] = {0.f, 0.f, 0.f, 0.f};
+  const long long n_units = (long long)a.tokens * heads;
+  for (long long u = (long long)(blockIdx.x - first) * WARPS + warp; u < n_units; u += (long long)blocks * WARPS) {
+    const int t = (int)(u / heads), h = (int)(u - (long long)t * heads);
+    const int pos = checked_position(a.positions[t], a.max_pos, a.status, lane == 0);
+    const T *xr = x + (size_t)t * x_stride + (size_t)h * a.hd, *dr = dy + ((size_t)t * heads + h) * a.hd;
+    T *o = dx + ((size_t)t * heads + h) * a.hd;
+    float z0[4], z1[4], x0[4], x1[4], ss = 0.f, dot = 0.f;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int i = lane + 32 * j;
-      if (i < half) { rb_red[warp * a.hd + i] = a0[j]; rb_red[warp * a.hd + i + half] = a1[j]; }
+      z0[j] = z1[j] = x0[j] = x1[j] = 0.f;
+      if (i < half) {
+        const float c = a.cos_tab[(size_t)pos * half + i], s = a.sin_tab[(size_t)pos * half + i];
+        const float d0 = to_f(dr[i]), d1 = to_f(dr[i + half]);
+        z0[j] = d0 * c + d1 * s;
+        z1[j] = d1 * c - d0 * s;
+        if (gain) {
+          x0[j] = to_f(xr[i]);
+          x1[j] = to_f(xr[i + half]);
+          ss = fmaf(x0[j], x0[j], fmaf(x1[j], x1[j], ss));
+          dot = fmaf(z0[j] * to_f(gain[i]), x0[j], fmaf(z1[j] * to_f(gain[i + half]), x1[j], dot));
+        }
+      }
     }
-    __syncthreads();
-    for (int i = threadIdx.x; i < a.hd; i += RB_THREADS) {
-      float v = 0.f;
-      for (int w = 0; w < WARPS; ++w) v += rb_red[w * a.hd + i];
-      a.partial[((size_t)blockIdx.x * 2 + which) * a.hd + i] = v;
+    float r = 1.f, m = 0.f;
+    if (gain) {
+      r = rsqrtf(warp_sum(ss) / a.hd + a.eps);
+      m = warp_sum(dot) * r * r / a.hd;
     }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int i = lane + 32 * j;
+      if (i >= half) continue;
+      float y0 = z0[j], y1 = z1[j];
+      if (gain) {
+        a0[j] = fmaf(z0[j], x0[j] * r, a0[j]);
+        a1[j] = fmaf(z1[j], x1[j] * r, a1[j]);
+        y0 = r * fmaf(-x0[j], m, z0[j] * to_f(gain[i]));
+        y1 = r * fmaf(-x1[j], m, z1[j] * to_f(gain[i + half]));
+      }
+      o[i] = round_to<T>(y0);
+      o[i + half] = round_to<T>(y1);
+    }
+  }
+  if (!gain) return;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int i = lane + 32 * j;
+    if (i < half) { rb_red[warp * a.hd + i] = a0[j]; rb_red[warp * a.hd + i + half] = a1[j]; }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < a.hd; i += RB_THREADS) {
+    float v = 0.f;
+    for (int w = 0; w < WARPS; ++w) v += rb_red[w * a.hd + i];
+    a.partial[(size_t)blockIdx.x * a.hd + i] = v;
   }
 }
 
-// gain gradients: block (32 elements, q or k) adds the blocks' partial sums, eight rows of warps side by side, in a fixed order
-__global__ void __launch_bounds__(256) gain_grad_kernel(const float *__restrict__ partial, int blocks, int hd, float *__restrict__ dq_gain,
-                                                        float *__restrict__ dk_gain) {
-  __shared__ float red[8][33];
-  const int which = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, i = blockIdx.x * 32 + lane;
-  float *dst = which ? dk_gain : dq_gain;
+// gain gradients: block (32 elements, q or k) adds the blocks' partial sums, 32 rows of warps side by side, in a fixed order (one row of
+// eight warps took 7 us for 296 blocks, most of it waiting)
+constexpr int GG_WARPS = 32;
+__global__ void __launch_bounds__(32 * GG_WARPS) gain_grad_kernel(const float *__restrict__ partial, int q_blocks, int blocks, int hd,
+                                                                 float *__restrict__ dq_gain, float *__restrict__ dk_gain) {
+  __shared__ float red[GG_WARPS][33];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, i = blockIdx.x * 32 + lane;
+  float *dst = blockIdx.y ? dk_gain : dq_gain;
   if (!dst) return;
+  const int end = blockIdx.y ? blocks : q_blocks;
   float v = 0.f;
   if (i < hd)
 #pragma unroll 8
-    for (int b = warp; b < blocks; b += 8) v += partial[((size_t)b * 2 + which) * hd + i];
+    for (int b = (blockIdx.y ? q_blocks : 0) + warp; b < end; b += GG_WARPS) v += partial[(size_t)b * hd + i];
   red[warp][lane] = v;
   __syncthreads();
   if (warp == 0 && i < hd) {
     float s = 0.f;
 #pragma unroll
-    for (int w = 0; w < 8; ++w) s += red[w][lane];
+    for (int w = 0; w < GG_WARPS; ++w) s += red[w][lane];
     dst[i] = s;
   }
 }
@@ -477,17 +593,30 @@ template <typename T>
 cudaError_t launch_qk_rope(const RopeArgs &a, cudaStream_t st) {
   const bool fp8 = a.k_scale != nullptr;
   if constexpr (sizeof(T) == 2) {
-    const bool vec = !fp8 && (a.hd == 64 || a.hd == 128 || a.hd == 256) && aligned16(a.q) && aligned16(a.k) && aligned16(a.v) && aligned16(a.q_out) &&
-                     aligned16(a.k_out) && aligned16(a.v_out) && aligned16(a.q_gain) && aligned16(a.k_gain) && aligned16(a.cos_tab) &&
-                     aligned16(a.sin_tab) && ((a.q_stride | a.k_stride | a.v_stride | a.qo_stride) & 7) == 0;
+    const int lanes = a.hd / 16;
+    bool vec = (a.hd == 64 || a.hd == 128 || a.hd == 256) && aligned16(a.q) && aligned16(a.k) && aligned16(a.v) && aligned16(a.q_out) &&
+               aligned16(a.k_out) && aligned16(a.v_out) && aligned16(a.q_gain) && aligned16(a.k_gain) && aligned16(a.cos_tab) &&
+               aligned16(a.sin_tab) && ((a.q_stride | a.k_stride | a.v_stride | a.qo_stride) & 7) == 0;
+    int row_lanes = lanes;
+    while (row_lanes < a.n_kv * lanes) row_lanes *= 2;
+    const int threads = rv_threads(fp8);
+    vec = vec && !(fp8 && row_lanes > threads);                // (an FP8 row's maximum is taken over one block's registers)
     if (vec) {
-      const int lanes = a.hd / 16, units = a.n_q + 2 * a.n_kv;
-      int threads = (units + 2) / 3 * lanes;               // three heads per thread
-      threads = (threads + 31) / 32 * 32;
-      if (threads > 512) threads = 512;
-      if (a.hd == 64) qk_norm_rope_vec_kernel<T, 4, 3><<<a.tokens, threads, 0, st>>>(a);
-      else if (a.hd == 128) qk_norm_rope_vec_kernel<T, 8, 3><<<a.tokens, threads, 0, st>>>(a);
-      else qk_norm_rope_vec_kernel<T, 16, 3><<<a.tokens, threads, 0, st>>>(a);
+      const int groups = threads / lanes, all = num_sms() * rv_blocks_per_sm(fp8), heads = a.n_q + 2 * a.n_kv;
+      auto share = [&](int n) {                                // blocks for n heads a token
+        const long long want = ((long long)a.tokens * n + groups - 1) / groups, most = (long long)all * n / heads;
+        return (int)(want < most ? want : most > 0 ? most : 1);
+      };
+      const int qb = share(a.n_q), kb = fp8 ? 0 : share(a.n_kv), per = threads / row_lanes;
+      const long long rest = fp8 ? (2ll * a.tokens + per - 1) / per : share(a.n_kv);
+      const unsigned grid = (unsigned)(qb + kb + rest);
+#define SKV_ROPE_VEC(LANES)                                                                                \
+  (fp8 ? qk_norm_rope_vec_kernel<T, LANES, true><<<grid, threads, 0, st>>>(a, qb, kb, row_lanes)        \
+       : qk_norm_rope_vec_kernel<T, LANES, false><<<grid, threads, 0, st>>>(a, qb, kb, row_lanes))
+      if (a.hd == 64) SKV_ROPE_VEC(4);
+      else if (a.hd == 128) SKV_ROPE_VEC(8);
+      else SKV_ROPE_VEC(16);
+#undef SKV_ROPE_VEC
       return cudaGetLastError();
     }
   }
@@ -501,26 +630,28 @@ int bwd_blocks() { return num_sms() * RB_BLOCKS_PER_SM; }
 template <typename T>
 cudaError_t launch_qk_rope_bwd(const RopeBwdArgs &a, float *dq_gain, float *dk_gain, cudaStream_t st) {
   bool vec = false;
-  const int lanes = a.hd / 16;
   if constexpr (sizeof(T) == 2) {
     vec = (a.hd == 64 || a.hd == 128 || a.hd == 256) && aligned16(a.q) && aligned16(a.k) && aligned16(a.dq) && aligned16(a.dk) && aligned16(a.dq_in) &&
           aligned16(a.dk_in) && aligned16(a.q_gain) && aligned16(a.k_gain) && aligned16(a.cos_tab) && aligned16(a.sin_tab) &&
           ((a.q_stride | a.k_stride) & 7) == 0;
   }
-  const long long per_block = vec ? RB_THREADS / lanes : RB_THREADS / 32;
-  const long long want = ((long long)a.tokens * a.n_q + per_block - 1) / per_block;
-  const int blocks = (int)(want < bwd_blocks() ? want : bwd_blocks());
+  const int per_block = vec ? RB_THREADS / (a.hd / 16) : RB_THREADS / 32;
+  auto share = [&](int n) {                                  // blocks for n heads a token
+    const long long want = ((long long)a.tokens * n + per_block - 1) / per_block, most = (long long)bwd_blocks() * n / (a.n_q + a.n_kv);
+    return (int)(want < most ? want : most > 0 ? most : 1);
+  };
+  const int qb = share(a.n_q), blocks = qb + share(a.n_kv);
   if constexpr (sizeof(T) == 2) {
     if (vec) {
-      if (a.hd == 64) qk_norm_rope_bwd_vec_kernel<T, 4><<<blocks, RB_THREADS, 0, st>>>(a);
-      else if (a.hd == 128) qk_norm_rope_bwd_vec_kernel<T, 8><<<blocks, RB_THREADS, 0, st>>>(a);
-      else qk_norm_rope_bwd_vec_kernel<T, 16><<<blocks, RB_THREADS, 0, st>>>(a);
+      if (a.hd == 64) qk_norm_rope_bwd_vec_kernel<T, 4><<<blocks, RB_THREADS, 0, st>>>(a, qb);
+      else if (a.hd == 128) qk_norm_rope_bwd_vec_kernel<T, 8><<<blocks, RB_THREADS, 0, st>>>(a, qb);
+      else qk_norm_rope_bwd_vec_kernel<T, 16><<<blocks, RB_THREADS, 0, st>>>(a, qb);
     }
   }
-  if (!vec) qk_norm_rope_bwd_kernel<T><<<blocks, RB_THREADS, (size_t)(RB_THREADS / 32) * a.hd * sizeof(float), st>>>(a);
+  if (!vec) qk_norm_rope_bwd_kernel<T><<<blocks, RB_THREADS, (size_t)(RB_THREADS / 32) * a.hd * sizeof(float), st>>>(a, qb);
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess || (!dq_gain && !dk_gain)) return e;
-  gain_grad_kernel<<<dim3((a.hd + 31) / 32, 2), 256, 0, st>>>(a.partial, blocks, a.hd, dq_gain, dk_gain);
+  gain_grad_kernel<<<dim3((a.hd + 31) / 32, 2), 32 * GG_WARPS, 0, st>>>(a.partial, qb, blocks, a.hd, dq_gain, dk_gain);
   return cudaGetLastError();
 }
 
@@ -573,7 +704,7 @@ extern "C" int32_t swiftkv_qk_norm_rope(const void *q, int64_t q_stride, const v
 
 extern "C" size_t swiftkv_qk_norm_rope_bwd_scratch_bytes(int32_t head_dim) {
   if (head_dim < 2 || head_dim > 256) return 0;
-  return (size_t)bwd_blocks() * 2 * head_dim * sizeof(float);
+  return (size_t)(bwd_blocks() + 1) * head_dim * sizeof(float);      // (at least one block each for queries and keys)
 }
 
 extern "C" int32_t swiftkv_qk_norm_rope_bwd(const void *dq, const void *dk, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
