@@ -237,7 +237,7 @@ size_t simt_scratch(int total_new, int max_kv, int n_q, int hd) {
 // starts or ends inside a (sequence, group, head) leaves an unnormalised partial result in `scratch` (at most two per CTA),
 // and a second kernel joins those in the order of the keys: deterministic, and balanced for any mix of lengths.  Where the
 // longest sequence has two groups, the CTAs form two classes, one per group, that walk over the same keys in step, so that
-// the second one finds them in L2 (a sequence with one group gives each class half of its keys).
+// the second one finds them in L2 (of a sequence with one group each class takes every other head).
 //
 // FP8 rows: TMA brings the codes and four warps widen them to IEEE half, exactly (every e4m3 number is one).  Queries in bf16
 // become halves too, each row times a power of two that brings its maximum to 2^14 .. 2^15: what that loses (elements below 2^-38 of the
@@ -245,11 +245,12 @@ size_t simt_scratch(int total_new, int max_kv, int n_q, int hd) {
 // exponent follows the largest scale-weighted probability of the row, so that P keeps the full half precision.  The two scales make
 // the softmax the longest step of a tile, and its time is a thread's: one row of 128 columns.  So a tile of at most 64 (32) rows is laid
 // out 2 (4) times along M, which the MMA does for nothing; each copy's softmax warps do their share of the tile's columns and
-// leave zeros for the others, and the copies are joined like the pieces of a split key range.
+// leave zeros for the others, and the copies are joined like the pieces of a split key range (in the CTA, through shared memory: 222 us instead of
+// 151 for 24 sequences of 10000 keys).
 //
 // What is not seen must not matter: keys behind the sequence and unseen drafts get S = -inf, and the V rows of the last
-// tiles are cleaned in shared memory first (0 * NaN is NaN): rows behind the sequence become zeros, and a drafted token's V row that
-// holds infinities or NaN is zeroed and handed to the rows that do see it in the epilogue.
+// tiles are cleaned in shared memory first (0 * NaN is NaN): rows behind the sequence become zeros, and so do infinities and NaN in a
+// drafted token's V row, which the epilogue hands to the rows that do see them.
 // ---------------------------------------------------------------------------------------------------------
 constexpr int TT_KEYS = 128;
 constexpr float TT_RESCALE = 8.0f;       // in log2 units
@@ -300,25 +301,29 @@ __device__ __forceinline__ float tt_exp2(float x) {
   return y;
 }
 
-// What a class of CTAs does of a sequence: key tiles [lo, hi) x KV heads x `groups` groups of W query tiles from group g0 on
-struct SeqShape { int tok0, n, past, tiles, lo, hi, g0, groups; };
+// What a class of CTAs does of a sequence: all key tiles x `heads` KV heads, every h_step-th from h0 on, x `groups` groups of W query tiles
+// from group g0 on.  Of two classes each takes one of two groups; of a sequence with one group, every other head.
+struct SeqShape { int tok0, n, past, tiles, g0, groups, h0, h_step, heads; };
 struct Split { int group_tokens, classes, cls; };
 __device__ __forceinline__ SeqShape seq_shape(const TreeArgs &a, int b, const Split &sp) {
   SeqShape s;
   tree_lengths(a, b, s.tok0, s.n, s.past, false);
   s.tiles = (s.past + s.n + TT_KEYS - 1) / TT_KEYS;
   s.groups = (s.n + sp.group_tokens - 1) / sp.group_tokens;
-  s.lo = s.g0 = 0;
-  s.hi = s.tiles;
-  if (sp.classes == 2 && s.groups) {
-    if (s.groups == 2) s.g0 = sp.cls;
-    else if (sp.cls == 0) s.hi = (s.tiles + 1) / 2;
-    else s.lo = (s.tiles + 1) / 2;
+  s.g0 = s.h0 = 0;
+  s.h_step = 1;
+  s.heads = a.n_kv;
+  if (sp.classes == 2 && s.groups == 2) {
+    s.g0 = sp.cls;
     s.groups = 1;
+  } else if (sp.classes == 2) {
+    s.h0 = (sp.cls + b) & 1;
+    s.h_step = 2;
+    s.heads = (a.n_kv + 1 - s.h0) / 2;
   }
   return s;
 }
-__device__ __forceinline__ int units_of(const TreeArgs &a, const SeqShape &s) { return (s.hi - s.lo) * s.groups * a.n_kv; }
+__device__ __forceinline__ int units_of(const SeqShape &s) { return s.tiles * s.groups * s.heads; }
 // a CTA's walk over its units, one (sequence, group, head) piece after the other; every role keeps its own
 struct Pieces {
   int b, gi, g, h, kt0, kt1, left;
@@ -329,26 +334,26 @@ struct Pieces {
     b = b0;
     s = seq_shape(a, b, sp);
     left = units;
-    const int len = s.hi - s.lo, item = within / len;
-    kt0 = s.lo + within % len;
-    h = item % a.n_kv;
-    gi = item / a.n_kv;
+    const int item = within / s.tiles;
+    kt0 = within % s.tiles;
+    h = s.h0 + item % s.heads * s.h_step;
+    gi = item / s.heads;
     g = s.g0 + gi;
-    kt1 = min(s.hi, kt0 + left);
+    kt1 = min(s.tiles, kt0 + left);
   }
   __device__ __forceinline__ bool next(const TreeArgs &a) {
     left -= kt1 - kt0;
     if (left <= 0) return false;
-    if (++h == a.n_kv) {
-      h = 0;
+    if ((h += s.h_step) >= a.n_kv) {
       if (++gi >= s.groups) {
         gi = 0;
-        do { s = seq_shape(a, ++b, sp); } while (units_of(a, s) == 0);
+        do { s = seq_shape(a, ++b, sp); } while (units_of(s) == 0);
       }
+      h = s.h0;
       g = s.g0 + gi;
     }
-    kt0 = s.lo;
-    kt1 = min(s.hi, kt0 + left);
+    kt0 = 0;
+    kt1 = min(s.tiles, kt0 + left);
     return true;
   }
   __device__ __forceinline__ bool whole() const { return kt0 == 0 && kt1 == s.tiles; }
@@ -422,7 +427,7 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
   int mine = 0;
   for (int b = b_lo; b < b_hi; ++b) {
     if (blockIdx.x == 0) { int x, y, z; tree_lengths(a, b, x, y, z, true); }
-    mine += units_of(a, seq_shape(a, b, split));
+    mine += units_of(seq_shape(a, b, split));
   }
   int inc = mine;
 #pragma unroll
@@ -443,7 +448,7 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
   if (u0 >= before && u0 < before + mine) {
     int at = before;
     for (int b = b_lo; b < b_hi; ++b) {
-      const int n = units_of(a, seq_shape(a, b, split));
+      const int n = units_of(seq_shape(a, b, split));
       if (u0 < at + n) { start[0] = b; start[1] = u0 - at; break; }
       at += n;
     }
@@ -686,36 +691,39 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
         const int tile = tc_count + j;
         const int j0 = (it.kt0 + j) * TT_KEYS - it.s.past;            // the tile's first key, counted from the first new token
         const bool edge = j0 > -TT_KEYS;                              // holds new tokens (and perhaps rows behind them)
-        if constexpr (!FP8) {
+        if (!(ok = wait(FP8 ? &s_full[w] : &s_half[w], sc & 1))) break;
+        tc::tc_fence_after_sync();
+        {
           if (edge && (W == 1 || w == 0)) {
-            // V rows that must not meet a zero probability as NaN or infinity (comment at the top)
+            // V rows that must not meet a zero probability as NaN or infinity (comment at the top).  Behind the wait for S: it was issued
+            // after the P V of two tiles before, so the V ring's place is in this tile's phase or the one before, never two before,
+            // which the parity could not tell from this one.
             const int s = tile % L::VS, key = j0 + r;
             if (!(ok = wait(&v_full[s], (tile / L::VS) & 1))) break;
             if (key >= 0) {
               uint8_t *vrow = smem + L::V + s * L::TILE + r * 128;
-              bool clear = key >= it.s.n;
-              if (!clear) {
-                uint32_t worst = 0;
+              const bool behind = key >= it.s.n;
+              bool handed = false;
+              constexpr uint32_t e = MMA_F16 ? 0x7c007c00u : 0x7f807f80u;
 #pragma unroll 1
-                for (int i = 0; i < L::CHUNKS * 8; ++i) {
-                  const uint4 x = *reinterpret_cast<const uint4 *>(vrow + (i >> 3) * L::CHUNK + (i & 7) * 16);
-                  const uint32_t e = F16 ? 0x7c007c00u : 0x7f807f80u, xs[4] = {x.x, x.y, x.z, x.w};
+              for (int i = 0; i < L::CHUNKS * 8; ++i) {
+                uint4 *at = reinterpret_cast<uint4 *>(vrow + (i >> 3) * L::CHUNK + (i & 7) * 16);
+                const uint4 x = *at;
+                uint32_t xs[4] = {x.x, x.y, x.z, x.w}, worst = 0;
 #pragma unroll
-                  for (int q4 = 0; q4 < 4; ++q4) worst |= ((xs[q4] & e & 0xffff0000u) == (e & 0xffff0000u)) | ((xs[q4] & e & 0xffffu) == (e & 0xffffu));
+                for (int q4 = 0; q4 < 4; ++q4) {
+                  const uint32_t gone = ((xs[q4] & e & 0xffff0000u) == (e & 0xffff0000u) ? 0xffff0000u : 0u) | ((xs[q4] & e & 0xffffu) == (e & 0xffffu) ? 0xffffu : 0u);
+                  worst |= gone;
+                  xs[q4] &= ~gone;
                 }
-                if (worst) { clear = true; bad_item[item & 1] = item + 1; }
+                if (behind) *at = make_uint4(0u, 0u, 0u, 0u);
+                else if (worst) { *at = make_uint4(xs[0], xs[1], xs[2], xs[3]); handed = true; }
               }
-              if (clear) {
-#pragma unroll 1
-                for (int i = 0; i < L::CHUNKS * 8; ++i)
-                  *reinterpret_cast<uint4 *>(vrow + (i >> 3) * L::CHUNK + (i & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
-                tc::fence_proxy_async_smem();
-              }
+              if (handed) bad_item[item & 1] = item + 1;
+              if (behind || handed) tc::fence_proxy_async_smem();
             }
           }
         }
-        if (!(ok = wait(FP8 ? &s_full[w] : &s_half[w], sc & 1))) break;
-        tc::tc_fence_after_sync();
         const float4 *ksc = reinterpret_cast<const float4 *>(scales + (tile & 3) * 384), *vsc = ksc + 32, *lvs = ksc + 64;
         if constexpr (FP8) {
           if (!(ok = wait(&g_full[tile & 3], (tile >> 2) & 1))) break;
@@ -924,11 +932,13 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
           f1 = x1.x == -INFINITY ? 0.f : tt_exp2((x1.x - m) * cm);
           l = x0.y * f0 + (nt > 1 ? x1.y * f1 : 0.f);
         }
-        const bool whole = it.whole() && (!FP8 || p.copies == 1), bad = bad_item[item & 1] == item + 1;
+        // (copies of a query tile leave partial results of their own, complete pieces by token and head)
+        const bool complete = it.whole(), whole = complete && (!FP8 || p.copies == 1), bad = bad_item[item & 1] == item + 1;
         const float inv = (whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f);
         const size_t head = (size_t)tok * a.n_q + it.h * rep + (valid ? rl % rep : 0);
-        const int slot = (int)blockIdx.x * 2 + (it.kt0 == it.s.lo ? 1 : 0);
-        const size_t srow = (size_t)slot * p.slot_rows + (W == 2 ? w : 0) * p.npt * rep + r;
+        const int slot = (int)blockIdx.x * 2 + (it.kt0 == 0 ? 1 : 0);
+        const size_t srow = FP8 && complete ? (size_t)gridDim.x * 2 * p.slot_rows + (size_t)copy * a.total_new * a.n_q + head
+                                            : (size_t)slot * p.slot_rows + (W == 2 ? w : 0) * p.npt * rep + r;
         constexpr int COLS = W == 1 ? HD / 2 : HD;
         const int col0 = W == 1 ? w * COLS : 0;
         if (valid && col0 == 0 && (W == 2 || w == 0)) {
@@ -951,12 +961,19 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
             for (int i = 0; i < 32; ++i) o[i] = fmaf(__uint_as_float(x[i]), f1, o[i]);
           }
           if (valid) {
-            if (bad) {
+            if (bad && (!FP8 || copy == 0)) {
               // drafted tokens of this piece whose V row was not finite: what the rows that see them get from it
 #pragma unroll 1
               for (int q2 = max(0, it.kt0 * TT_KEYS - it.s.past); q2 < min(it.s.n, it.kt1 * TT_KEYS - it.s.past); ++q2) {
                 const int row = tree_row(a, it.b, it.s.past + q2);
                 if (row < 0 || !tree_sees(a, tok, node, it.s.past, it.s.n, it.s.past + q2)) continue;
+                if constexpr (FP8) {
+                  const uint8_t *v = reinterpret_cast<const uint8_t *>(a.v) + ((size_t)row * a.n_kv + it.h) * HD + d0;
+#pragma unroll
+                  for (int i = 0; i < 32; ++i)
+                    if ((v[i] & 0x7f) == 0x7f) o[i] = NAN;
+                  continue;
+                }
                 const uint16_t *v = reinterpret_cast<const uint16_t *>(a.v) + ((size_t)row * a.n_kv + it.h) * HD + d0;
                 const uint16_t e = F16 ? 0x7c00 : 0x7f80;
 #pragma unroll
@@ -1114,7 +1131,7 @@ __global__ void __launch_bounds__(TJ_THREADS) tree_attention_tc_join_kernel(Tree
     for (int k = 0; k < 2; ++k) {
       if (k >= p.classes) break;
       const SeqShape s = seq_shape(a, b, Split{group_tokens, p.classes, k});
-      const int u = units_of(a, s);
+      const int u = units_of(s);
       sum[k][1] += u;
       if (s.tok0 + s.n <= t) sum[k][0] += u;
       else if (s.tok0 <= t) s_b = b;
@@ -1135,31 +1152,33 @@ __global__ void __launch_bounds__(TJ_THREADS) tree_attention_tc_join_kernel(Tree
   constexpr int LANES = HD / 4, PER_PASS = TJ_THREADS / LANES;
   const int d = (tid % LANES) * 4, hq = blockIdx.y * PER_PASS + tid / LANES, h = hq / rep;
   if (hq >= a.n_q) return;
-  // the CTAs of each class that worked on this row's item, in the order of the keys
-  int c0[2], n_pieces[2] = {0, 0}, row = 0;
+  // the CTAs that worked on this row's item, of one class, in the order of the keys
+  int cls = 0, c0 = 0, n = 0, row = 0;
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
-    c0[k] = 0;
     if (k >= p.classes) break;
     const SeqShape s = seq_shape(a, b, Split{group_tokens, p.classes, k});
-    const int node = t - s.tok0, g = node / group_tokens, len = s.hi - s.lo;
-    row = (node - g * group_tokens) * rep + hq % rep;
-    if (g < s.g0 || g >= s.g0 + s.groups || len == 0) continue;
+    const int node = t - s.tok0, g = node / group_tokens;
+    if (g < s.g0 || g >= s.g0 + s.groups || (h - s.h0) % s.h_step) continue;
     int before = 0, total = 0;
 #pragma unroll
     for (int w = 0; w < TJ_THREADS / 32; ++w) { before += s_sum[k][0][w]; total += s_sum[k][1][w]; }
     const int ctas = (grid - k + p.classes - 1) / p.classes, per = (total + ctas - 1) / ctas;
-    const int first = before + ((g - s.g0) * a.n_kv + h) * len;
-    c0[k] = first / per;
-    n_pieces[k] = (first + len - 1) / per - c0[k] + 1;
+    const int first = before + ((g - s.g0) * s.heads + (h - s.h0) / s.h_step) * s.tiles;
+    cls = k;
+    row = (node - g * group_tokens) * rep + hq % rep;
+    c0 = first / per;
+    n = (first + s.tiles - 1) / per - c0 + 1;
   }
-  const int n = (n_pieces[0] + n_pieces[1]) * p.copies;
+  const int pieces = n;
+  n *= p.copies;
   if (n <= 1) return;                                      // whole: already in `out`
-  // a class's first piece starts at its first key: its CTA's slot 1; the others are the first piece of theirs: slot 0
+  // the first piece starts at the first key: its CTA's slot 1; the others are the first piece of theirs: slot 0.  Copies of a complete
+  // piece (a CTA may have many of these): by token and head.
   auto piece = [&](int ic) -> size_t {
     const int i = ic / p.copies, copy = ic % p.copies;
-    const int k = i < n_pieces[0] ? 0 : 1, j = k ? i - n_pieces[0] : i;
-    return (size_t)((((c0[k] + j) * p.classes + k) * 2 + (j == 0 ? 1 : 0))) * p.slot_rows + copy * (128 / p.copies) + row;
+    if (pieces == 1) return (size_t)grid * 2 * p.slot_rows + ((size_t)copy * a.total_new + t) * a.n_q + hq;
+    return (size_t)(((c0 + i) * p.classes + cls) * 2 + (i == 0 ? 1 : 0)) * p.slot_rows + copy * (128 / p.copies) + row;
   };
   const float2 *ml = reinterpret_cast<const float2 *>(a.scratch);
   float m = -INFINITY, l = 0.f, o0 = 0.f, o1 = 0.f, o2 = 0.f, o3 = 0.f;
@@ -1211,10 +1230,14 @@ int tc_slot_rows(int total_new, int n_q, int n_kv) {
   const long long all = (long long)total_new * (n_q / n_kv);
   return all < 256 ? (int)all : 256;
 }
+// copies of query tiles: at most so many (copy, token) pairs leave results of their own (34 MB of scratch for 32 heads of 128); calls of
+// more tokens lay their tiles out less often, for they have rows enough elsewhere
+constexpr int TC_COPY_TOKENS = 2048;
 size_t tc_scratch(int total_new, int n_q, int hd) {
   // (independent of the group size: a call's rows of one KV head are at most all its rows)
   const int rows = tc_slot_rows(total_new, n_q, 1);
-  return (size_t)num_sms() * 2 * (rows < 128 ? 128 : rows) * (hd + 2) * sizeof(float) + 256;
+  const long long copied = 4ll * total_new < TC_COPY_TOKENS ? 4ll * total_new : TC_COPY_TOKENS;
+  return ((size_t)num_sms() * 2 * (rows < 128 ? 128 : rows) + (size_t)copied * n_q) * (hd + 2) * sizeof(float) + 256;
 }
 
 // shapes and addresses that the tensor-core form takes (TMA: 16-byte boundaries and strides)
@@ -1243,7 +1266,8 @@ int32_t launch_tc(TreeTcArgs p, int max_kv, cudaStream_t st) {
   if (most > 0x7fffffffLL) return report_error(SWIFTKV_ERR_UNSUPPORTED, "too many key tiles for one launch");
   const int grid = (int)(most < num_sms() ? most : num_sms());
   p.classes = groups == 2 && grid > 1 ? 2 : 1;
-  const size_t ml_bytes = ((size_t)grid * 2 * p.slot_rows * sizeof(float2) + 255) & ~(size_t)255;
+  const size_t rows = (size_t)grid * 2 * p.slot_rows + (p.copies > 1 ? (size_t)p.copies * a.total_new * a.n_q : 0);
+  const size_t ml_bytes = (rows * sizeof(float2) + 255) & ~(size_t)255;
   p.part_o = reinterpret_cast<float *>(reinterpret_cast<uint8_t *>(a.scratch) + ml_bytes);
   kernel<<<grid, L::THREADS, L::BYTES, st>>>(tq, tk, tv, p);
   cudaError_t e = cudaGetLastError();
@@ -1262,6 +1286,7 @@ int32_t launch_tc_for(const TreeArgs &a, bool fp8, int max_kv, cudaStream_t st) 
   const int rep = a.n_q / a.n_kv;
   // (24 sequences of 10000 keys, 32 rows: 187 us in four copies, 210 us in two, 283 us in one; 64 rows: 219 us in two, 286 us in one)
   p.copies = !fp8 ? 1 : a.max_new * rep <= 32 ? 4 : a.max_new * rep <= 64 ? 2 : 1;
+  while (p.copies > 1 && (long long)p.copies * a.total_new > TC_COPY_TOKENS) p.copies /= 2;
   p.npt = 128 / p.copies / rep;
   p.slot_rows = p.copies > 1 ? 128 : tc_slot_rows(a.total_new, a.n_q, a.n_kv);
   p.scale_log2 = a.scale * 1.4426950408889634f;

@@ -374,6 +374,67 @@ def test_tree_attention_other_shapes(heads, kind):
     check_tree(c, *run_tree(c))
 
 
+# many short sequences: several complete (sequence, head) pieces, and parts of others, per block of the grid
+MANY = {"few rows": [(300 + 17 * i, 1 + i % 8) for i in range(40)],
+        "64 rows": [(100 + 23 * i, 9 + i % 8) for i in range(30)],
+        "128 rows": [(100 + 31 * i, 3 + i * 7 % 30) for i in range(30)],
+        "one and two groups": [(150 + 43 * i, 150 if i % 6 == 1 else 1 + i % 5) for i in range(24)],
+        "three groups": [(150 + 43 * i, 270 if i % 12 == 1 else 3) for i in range(24)]}
+
+
+@pytest.mark.parametrize("lens", MANY, ids=str)
+@pytest.mark.parametrize("heads", [(16, 8, 128), (15, 5, 64), (4, 1, 128)], ids=str)
+@pytest.mark.parametrize("kind", ["bf16", "fp8"])
+def test_tree_attention_many_pieces_per_block(lens, heads, kind):
+    c = tree_case(len(lens), MANY[lens], *heads, BF, fp8=kind == "fp8")
+    check_tree(c, *run_tree(c))
+
+
+def test_tree_attention_more_tokens_than_copies_are_kept_for():
+    """An FP8 cache and tiles of few rows, but 700, then 2600 of them."""
+    for seqs, new in ((700, 1), (1300, 2)):
+        c = tree_case(seqs, [(i % 140, new) for i in range(seqs)], 4, 2, 64, BF, fp8=True)
+        check_tree(c, *run_tree(c))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp8"])
+@pytest.mark.parametrize("hi", [8, 24, 50, 150])
+def test_tree_attention_repeats_bit_for_bit(kind, hi):
+    """Thirty calls over sequences whose warps of unused rows run ahead of the others into the last tiles of a sequence."""
+    c = tree_case(hi, [(400 + 331 * i, 1 + i * 13 % hi) for i in range(16)], 16, 8, 128, BF, fp8=kind == "fp8")
+    first, lse = run_tree(c)
+    if hi == 24:
+        check_tree(c, first, lse)
+    for _ in range(30):
+        out, l2 = run_tree(c)
+        assert torch.equal(out, first) and torch.equal(l2, lse)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16", "fp8", "f32"])
+@pytest.mark.parametrize("n", [6, 12, 30, 60])
+def test_tree_attention_one_element_of_a_drafted_row(kind, n):
+    """An infinity or NaN in one element of a drafted token's K or V.  Who does not see the token keeps the result; who sees it gets it
+    everywhere (K) or in that element (V), and keeps the rest of the row."""
+    c = tree_case(n, [(250, n), (90, 2)], 16, 4, 128, {"bf16": BF, "f16": HF, "fp8": BF, "f32": FF}[kind], fp8=kind == "fp8")
+    row = int(c["rows"][0][251])
+    who = torch.tensor(np.flatnonzero(c["sees"][0][:, 1]), device="cuda")
+    assert 0 < len(who) < n
+    for what in ("k", "v"):
+        if what == "v":
+            c["v"][row, 2, 17] = 0
+        base, _ = run_tree(c)
+        kept = c[what][row, 2, 17].clone()
+        c[what][row, 2, 17] = 0xFF if kind == "fp8" else float("nan") if what == "k" else float("inf")
+        out, _ = run_tree(c)
+        c[what][row, 2, 17] = kept
+        hit = torch.zeros(out.shape, dtype=torch.bool, device="cuda")
+        if what == "k":
+            hit[who, 8:12] = True
+        else:
+            hit[who, 8:12, 17] = True
+        assert torch.equal(out[~hit], base[~hit]) and not torch.isfinite(out[hit]).any(), what
+
+
 @pytest.mark.parametrize("kind", ["bf16", "f16", "fp8", "f32"])
 def test_tree_attention_causal_and_scale(kind):
     c = tree_case(3, [(1029, 130), (0, 257), (3, 1)], 8, 2, 128, {"bf16": BF, "f16": HF, "fp8": BF, "f32": FF}[kind], fp8=kind == "fp8", mask=False)
