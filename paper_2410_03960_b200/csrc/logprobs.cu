@@ -391,8 +391,9 @@ __global__ void __launch_bounds__(LP_THREADS + 32, 2) token_logprobs_kernel(LpAr
       const float tgt_v = tgt >= 0 && tgt < a.vocab ? lp_load(x + tgt) : 0.f;
       const uint32_t done = tc::smem_u32(&sh.row_done[par]);
       const long long t0 = clock64();
-      while (alive && !tc::mbar_try_wait(done, (turn >> 1) & 1)) {
-        if (clock64() - t0 > tc::WAIT_LIMIT_CLOCKS) {
+      // (the lanes leave together: what is between the looks has the whole warp's shuffles)
+      while (alive && !__any_sync(0xffffffffu, tc::mbar_try_wait(done, (turn >> 1) & 1))) {
+        if (__any_sync(0xffffffffu, clock64() - t0 > tc::WAIT_LIMIT_CLOCKS)) {
           if (lane == 0) atomicOr(a.status, STATUS_TIMEOUT);
           alive = false;
         }

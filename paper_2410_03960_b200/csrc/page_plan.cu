@@ -28,7 +28,7 @@ struct PlanArgs {
 // lengths as the device finds them: counts below zero read as zero, entries in use are at most what a table row holds
 __device__ __forceinline__ void plan_lengths(const PlanArgs &a, int b, int &past, int &fresh, int &owned, int &need, int &lacking) {
   past = max(0, a.past[b]);
-  fresh = max(0, a.n_new[b]);
+  fresh = min(max(0, a.n_new[b]), 0x7fffffff - past);
   owned = min(max(0, a.owned[b]), a.max_blocks);
   const int wanted = (int)(((unsigned)past + (unsigned)fresh + PAGE_ROWS - 1) / PAGE_ROWS);
   need = max(0, min(wanted, a.max_blocks) - owned);
@@ -86,11 +86,11 @@ __global__ void __launch_bounds__(PP_THREADS) plan_pages_kernel(PlanArgs a) {
   const int n_free = min(max(0, *a.n_free), a.free_cap);
   const int taken = min(all.y, n_free);
   const int total = min(all.x, a.max_tokens);
-  // the page of table entry j of sequence b, -1 where it has none
+  // the page of table entry j of sequence b, -1 where it has none (j and the rank are negative where the sums of what was given wrap)
   auto page_of = [&](int b, int owned, int j) -> int {
-    if (j < owned) return a.table[(size_t)b * a.max_blocks + j];
+    if (j >= 0 && j < owned) return a.table[(size_t)b * a.max_blocks + j];
     const int rank = s_first[b] + j - owned;
-    return (j < a.max_blocks && rank < s_first[b + 1] && rank < n_free) ? a.free_pages[n_free - 1 - rank] : -1;
+    return (j >= owned && j < a.max_blocks && rank >= 0 && rank < s_first[b + 1] && rank < n_free) ? a.free_pages[n_free - 1 - rank] : -1;
   };
   // new tokens, one per thread: the sequence by a binary search in the offsets
   for (int t = blockIdx.x * PP_THREADS + tid; t < total; t += gridDim.x * PP_THREADS) {
@@ -101,7 +101,7 @@ __global__ void __launch_bounds__(PP_THREADS) plan_pages_kernel(PlanArgs a) {
     }
     const int pos = max(0, a.past[lo]) + t - s_cu[lo];
     const int page = page_of(lo, min(max(0, a.owned[lo]), a.max_blocks), pos / PAGE_ROWS);
-    a.slot_map[t] = page >= 0 ? page * PAGE_ROWS + pos % PAGE_ROWS : -1;
+    a.slot_map[t] = page >= 0 && page < 0x7fffffff / PAGE_ROWS ? page * PAGE_ROWS + pos % PAGE_ROWS : -1;
     a.positions[t] = pos;
   }
   // block tables, one warp per row; in place only the entries behind the used ones are written

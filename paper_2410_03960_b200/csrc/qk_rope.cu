@@ -566,11 +566,12 @@ __global__ void __launch_bounds__(RB_THREADS) qk_norm_rope_bwd_kernel(RopeBwdArg
 // gain gradients: block (32 elements, q or k) adds the blocks' partial sums, 32 rows of warps side by side, in a fixed order (one row of
 // eight warps took 7 us for 296 blocks, most of it waiting)
 constexpr int GG_WARPS = 32;
-__global__ void __launch_bounds__(32 * GG_WARPS) gain_grad_kernel(const float *__restrict__ partial, int q_blocks, int blocks, int hd,
+__global__ void __launch_bounds__(32 * GG_WARPS) gain_grad_kernel(const float *partial, int q_blocks, int blocks, int hd,
                                                                  float *__restrict__ dq_gain, float *__restrict__ dk_gain) {
   __shared__ float red[GG_WARPS][33];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, i = blockIdx.x * 32 + lane;
   float *dst = blockIdx.y ? dk_gain : dq_gain;
+  wait_for_previous();
   if (!dst) return;
   const int end = blockIdx.y ? blocks : q_blocks;
   float v = 0.f;
@@ -651,8 +652,7 @@ cudaError_t launch_qk_rope_bwd(const RopeBwdArgs &a, float *dq_gain, float *dk_g
   if (!vec) qk_norm_rope_bwd_kernel<T><<<blocks, RB_THREADS, (size_t)(RB_THREADS / 32) * a.hd * sizeof(float), st>>>(a, qb);
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess || (!dq_gain && !dk_gain)) return e;
-  gain_grad_kernel<<<dim3((a.hd + 31) / 32, 2), 32 * GG_WARPS, 0, st>>>(a.partial, qb, blocks, a.hd, dq_gain, dk_gain);
-  return cudaGetLastError();
+  return launch_early(gain_grad_kernel, dim3((a.hd + 31) / 32, 2), 32 * GG_WARPS, st, a.partial, qb, blocks, a.hd, dq_gain, dk_gain);
 }
 
 bool dtype_ok(int32_t d) { return d == SWIFTKV_DTYPE_F32 || d == SWIFTKV_DTYPE_BF16 || d == SWIFTKV_DTYPE_F16; }

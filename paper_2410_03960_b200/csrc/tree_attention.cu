@@ -442,6 +442,7 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
     if (w < warp) before += warp_sum_s[w];
     total += warp_sum_s[w];
   }
+  launch_dependents();
   const int per = (total + ctas - 1) / ctas;
   const int u0 = (int)min((long long)total, (long long)cta * per), units = min(total - u0, per);
   if (units <= 0) return;
@@ -1122,6 +1123,7 @@ __global__ void __launch_bounds__(TJ_THREADS) tree_attention_tc_join_kernel(Tree
   const TreeArgs &a = p.a;
   const int t = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int group_tokens = tiles_per_group * p.npt, rep = a.n_q / a.n_kv;
+  // (the lengths are the call's inputs: the sums over them run beside the pieces' kernel)
   __shared__ int s_sum[2][2][TJ_THREADS / 32], s_b;        // [class][before, total]
   if (tid == 0) s_b = -1;
   __syncthreads();
@@ -1147,6 +1149,7 @@ __global__ void __launch_bounds__(TJ_THREADS) tree_attention_tc_join_kernel(Tree
       if (lane == 0) s_sum[k][q][warp] = v;
     }
   __syncthreads();
+  wait_for_previous();
   const int b = s_b;
   if (b < 0) return;                                       // a row behind the last sequence
   constexpr int LANES = HD / 4, PER_PASS = TJ_THREADS / LANES;
@@ -1273,8 +1276,7 @@ int32_t launch_tc(TreeTcArgs p, int max_kv, cudaStream_t st) {
   cudaError_t e = cudaGetLastError();
   if (e == cudaSuccess && (grid > 1 || p.copies > 1)) {
     constexpr int PER_PASS = TJ_THREADS / (HD / 4);
-    tree_attention_tc_join_kernel<HD, F16><<<dim3(a.total_new, (a.n_q + PER_PASS - 1) / PER_PASS), TJ_THREADS, 0, st>>>(p, grid, W);
-    e = cudaGetLastError();
+    e = launch_early(tree_attention_tc_join_kernel<HD, F16>, dim3(a.total_new, (a.n_q + PER_PASS - 1) / PER_PASS), TJ_THREADS, st, p, grid, W);
   }
   return e == cudaSuccess ? SWIFTKV_OK : report_error(SWIFTKV_ERR_CUDA, cudaGetErrorString(e));
 }
