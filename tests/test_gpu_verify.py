@@ -86,6 +86,23 @@ def test_plan_pages_bounds_what_it_finds():
     assert slots[300:310] == [6 * 128 + 100 + i for i in range(10)]
 
 
+def test_plan_pages_follows_nothing_where_sums_wrap():
+    """Counts of new tokens that no memory could hold: rows stay inside the pages that are there, or are -1."""
+    import paper_2410_03960_b200 as P
+    for seqs in (3, 5):
+        table = torch.arange(seqs * 6, dtype=torch.int32, device="cuda").view(seqs, 6)
+        free = i32(range(100, 140))
+        out = P.plan_pages(i32([200] * seqs), i32([1 << 30] * seqs), i32([2] * seqs), table, free, i32([40]), max_tokens=700)
+        torch.cuda.synchronize()
+        out["slot_map"].fill_(-1)
+        P.plan_pages(i32([200] * seqs), i32([1 << 30] * seqs), i32([2] * seqs), table, free, i32([40]), out=out)
+        rows = out["slot_map"]
+        assert ((rows >= -1) & (rows < 140 * 128)).all()
+        bt = out["block_table"]
+        assert ((bt >= -1) & (bt < 140)).all()
+        assert torch.equal(bt[:, :2], table[:, :2])
+
+
 # ------------------------------------------------------------------------------------------- qk_norm_rope and gradient
 def rope_inputs(T, n_q, n_kv, hd, dt, seed, strided=True, max_pos=131072):
     g = torch.Generator(device="cuda").manual_seed(seed)
