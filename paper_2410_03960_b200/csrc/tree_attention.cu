@@ -180,7 +180,13 @@ __global__ void __launch_bounds__(TS_THREADS) tree_attention_simt_kernel(TreeArg
 template <typename TQ>
 __global__ void __launch_bounds__(TS_THREADS) tree_attention_join_kernel(TreeArgs a, int splits) {
   const int t = blockIdx.x / a.n_q;
-  if (t < a.cu[0] || t >= a.cu[a.n_seqs]) return;              // rows behind the last sequence stay as they were
+  int inside = 0;
+  for (int b = threadIdx.x; b < a.n_seqs; b += TS_THREADS) {
+    int tok0, n, past;
+    tree_lengths(a, b, tok0, n, past, false);
+    inside |= t >= tok0 && t < tok0 + n;
+  }
+  if (!__syncthreads_or(inside)) return;                       // rows of no sequence, and those cut off one, stay as they were
   const size_t head = blockIdx.x;
   const float *src = a.scratch + head * splits * (a.hd + 2);
   float M = -INFINITY, L = 0.f;

@@ -578,6 +578,22 @@ def test_tree_attention_reports_lengths_and_pages():
             P.op_status()
 
 
+@pytest.mark.parametrize("kind", ["bf16", "fp8", "f32"])
+@pytest.mark.parametrize("past", [50, 2100])
+def test_tree_attention_rows_cut_off_a_sequence(kind, past):
+    """A sequence of more new tokens than max_new: the rest of its rows stay as they were, and the call is reported."""
+    import paper_2410_03960_b200 as P
+    c = tree_case(past, [(past, 9), (40, 3)], 8, 2, 128, FF if kind == "f32" else BF, fp8=kind == "fp8", mask=False)
+    c["max_new"] = 5
+    out = torch.full(c["q"].shape, 5.0, dtype=c["dt"], device="cuda")
+    out, lse = run_tree(c, out=out)
+    assert (out[5:9] == 5).all() and (lse[5:9] == 77).all()
+    assert (out[:5] != 5).any(dim=-1).all() and (out[9:] != 5).any(dim=-1).all() and (lse[9:] != 77).all()
+    with pytest.raises(P.SwiftKVError) as e:
+        P.op_status()
+    assert e.value.code == -6
+
+
 def test_tree_attention_one_token_equals_tail_attention():
     """One new token per sequence is the single-query attention of the last-token path."""
     import paper_2410_03960_b200 as P
