@@ -254,6 +254,11 @@ size_t simt_scratch(int total_new, int max_kv, int n_q, int hd) {
 // leave zeros for the others, and the copies are joined like the pieces of a split key range (in the CTA, through shared memory: 222 us instead of
 // 151 for 24 sequences of 10000 keys).
 //
+// What bounds it: HBM for 16-bit caches and up to about 64 query rows per KV head (24 sequences of one token over 10000 keys 158 us,
+// 0.96 of the copy bandwidth; 16 of 9 to 32 tokens over 2048 to 8192 keys 70 us, 4.3 TB/s); each stream's chain of softmax, P V and next
+// Q K^T for two full tiles (2 x 64 tokens, 8 heads per KV head, over 131072 keys 470 - 520 us, 1.0 - 1.1 PFLOP/s); shared memory for FP8
+// caches (24 sequences of up to 8 tokens over up to 10000 keys 145 us, 2.5 TB/s); latency for few keys (1 token over 700 keys 12 us).
+//
 // What is not seen must not matter: keys behind the sequence and unseen drafts get S = -inf, and the V rows of the last
 // tiles are cleaned in shared memory first (0 * NaN is NaN): rows behind the sequence become zeros, and so do infinities and NaN in a
 // drafted token's V row, which the epilogue hands to the rows that do see them.
@@ -506,172 +511,172 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
 
   // FP8: 16 warps at 128 registers; what the copying and widening warps leave goes to the softmax warps (72 + 88 + 2 x 176 = 4 x 128)
   if (warp < L::SOFT) {
-  if constexpr (FP8) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-  if (warp == 0) {
-    if (lane == 0) {
-      // ------------------------------------------------------------------ K / V tiles (FP8: their codes, K and V in turn)
-      int kc = 0, vc = 0, cc = 0;
-      bool ok = true;
-      int entry = tile_entry(a, it.b, it.kt0);
-      do {
-        for (int j = it.kt0; j < it.kt1 && ok; ++j) {
-          const int now = tile_row(a, entry, j);
-          if (j + 1 < it.kt1) entry = tile_entry(a, it.b, j + 1);      // (the table's answer travels while this tile waits)
-          if constexpr (FP8) {
-            for (int kv = 0; kv < 2 && ok; ++kv, ++cc) {
-              const int s = cc % L::CS;
-              ok = wait(&c_empty[s], ((cc / L::CS) & 1) ^ 1);
+    if constexpr (FP8) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    if (warp == 0) {
+      if (lane == 0) {
+        // ------------------------------------------------------------------ K / V tiles (FP8: their codes, K and V in turn)
+        int kc = 0, vc = 0, cc = 0;
+        bool ok = true;
+        int entry = tile_entry(a, it.b, it.kt0);
+        do {
+          for (int j = it.kt0; j < it.kt1 && ok; ++j) {
+            const int now = tile_row(a, entry, j);
+            if (j + 1 < it.kt1) entry = tile_entry(a, it.b, j + 1);      // (the table's answer travels while this tile waits)
+            if constexpr (FP8) {
+              for (int kv = 0; kv < 2 && ok; ++kv, ++cc) {
+                const int s = cc % L::CS;
+                ok = wait(&c_empty[s], ((cc / L::CS) & 1) ^ 1);
+                if (!ok) break;
+                const uint32_t bar = tc::smem_u32(&c_full[s]);
+                tc::mbar_expect_tx(bar, L::CODE_TILE);
+                tc::tma_load_2d(tc::smem_u32(smem + L::C + s * L::CODE_TILE), kv ? &tmV : &tmK, bar, it.h * (HD / 2), now);
+              }
+            } else {
+              int s = kc % L::KS;
+              ok = wait(&k_empty[s], ((kc / L::KS) & 1) ^ 1);
               if (!ok) break;
-              const uint32_t bar = tc::smem_u32(&c_full[s]);
-              tc::mbar_expect_tx(bar, L::CODE_TILE);
-              tc::tma_load_2d(tc::smem_u32(smem + L::C + s * L::CODE_TILE), kv ? &tmV : &tmK, bar, it.h * (HD / 2), now);
+              uint32_t bar = tc::smem_u32(&k_full[s]);
+              tc::mbar_expect_tx(bar, L::TILE);
+              for (int c = 0; c < L::CHUNKS; ++c)
+                tc::tma_load_2d(tc::smem_u32(smem + L::K + s * L::TILE + c * L::CHUNK), &tmK, bar, it.h * HD + c * 64, now);
+              ++kc;
+              s = vc % L::VS;
+              ok = wait(&v_empty[s], ((vc / L::VS) & 1) ^ 1);
+              if (!ok) break;
+              bar = tc::smem_u32(&v_full[s]);
+              tc::mbar_expect_tx(bar, L::TILE);
+              for (int c = 0; c < L::CHUNKS; ++c)
+                tc::tma_load_2d(tc::smem_u32(smem + L::V + s * L::TILE + c * L::CHUNK), &tmV, bar, it.h * HD + c * 64, now);
+              ++vc;
             }
-          } else {
-            int s = kc % L::KS;
-            ok = wait(&k_empty[s], ((kc / L::KS) & 1) ^ 1);
-            if (!ok) break;
-            uint32_t bar = tc::smem_u32(&k_full[s]);
-            tc::mbar_expect_tx(bar, L::TILE);
-            for (int c = 0; c < L::CHUNKS; ++c)
-              tc::tma_load_2d(tc::smem_u32(smem + L::K + s * L::TILE + c * L::CHUNK), &tmK, bar, it.h * HD + c * 64, now);
-            ++kc;
-            s = vc % L::VS;
-            ok = wait(&v_empty[s], ((vc / L::VS) & 1) ^ 1);
-            if (!ok) break;
-            bar = tc::smem_u32(&v_full[s]);
-            tc::mbar_expect_tx(bar, L::TILE);
-            for (int c = 0; c < L::CHUNKS; ++c)
-              tc::tma_load_2d(tc::smem_u32(smem + L::V + s * L::TILE + c * L::CHUNK), &tmV, bar, it.h * HD + c * 64, now);
-            ++vc;
           }
-        }
-        if (!ok || !it.next(a)) break;
-        entry = tile_entry(a, it.b, it.kt0);
-      } while (true);
-    }
-  } else if (warp == 1) {
-    // -------------------------------------------------------------------- MMA issuer (one elected lane), query tiles
-    const bool leader = tc::elect_one();
-    constexpr int QK_PARTS = FP8 ? 1 : 2;       // (FP8: shared-memory bandwidth counts, and each part reads Q again)
-    constexpr uint32_t idesc_qk = tc::umma_idesc(128, TT_KEYS / QK_PARTS, 0, 0, MMA_F16, MMA_F16);
-    constexpr uint32_t idesc_pv = tc::umma_idesc(128, HD, 0, 1, MMA_F16, MMA_F16);
-    const uint64_t q_desc = tc::umma_desc_sw128(tc::smem_u32(smem + L::Q), 16, 1024);
-    const uint64_t k_desc = tc::umma_desc_sw128(tc::smem_u32(smem + L::K), 16, 1024);
-    const uint64_t v_desc = tc::umma_desc_sw128(tc::smem_u32(smem + L::V), L::CHUNK, 1024);
-    int kc = 0, vc = 0, item = 0, sc0 = 0, sc1 = 0;
-    bool ok = true, more;
-    auto load_q = [&]() {
-      const uint32_t bar = tc::smem_u32(q_full);
-      const int copies = FP8 ? p.copies : 1;
-      tc::mbar_expect_tx(bar, W * copies * L::CHUNKS * p.npt * rep * 128);
-      for (int w = 0; w < W; ++w)
-        for (int q = 0; q < copies; ++q)
-          for (int c = 0; c < L::CHUNKS; ++c)
-            tc::tma_load_3d(tc::smem_u32(smem + L::Q + w * L::TILE + c * L::CHUNK + q * (128 / copies) * 128), &tmQ, bar, c * 64, it.h * rep,
-                            it.s.tok0 + (it.g * W + w) * p.npt);
-    };
-    if (leader) load_q();
-    do {
-      const int nt = it.kt1 - it.kt0, steps = W == 2 ? 2 * nt : nt;
-      // S of a step; steps alternate between the streams.  The stream's last P V was issued before, and runs before.
-      auto issue_qk = [&](int step) -> bool {
-        const int w = step & 1, s = kc % L::KS;
-        if (W == 1 || w == 0) {
-          if (!wait(&k_full[s], (kc / L::KS) & 1)) return false;
-          tc::tc_fence_after_sync();
-        }
-        if (leader) {
-          // the scores of 64 keys after the other 64: the softmax warps start on the first half
-          const uint64_t qd = q_desc + (uint64_t)((W == 2 ? w : 0) * (L::TILE >> 4)), kd = k_desc + (uint64_t)(s * (L::TILE >> 4));
-#pragma unroll
-          for (int hf = 0; hf < QK_PARTS; ++hf) {
-#pragma unroll
-            for (int kk = 0; kk < HD / 16; ++kk) {
-              const uint32_t off = ((kk >> 2) * L::CHUNK + (kk & 3) * 32) >> 4;
-              tc::umma_ss(tmem_base + w * 128 + hf * 64, qd + off, kd + off + hf * (64 * 128 >> 4), idesc_qk, kk != 0);
-            }
-            tc::umma_commit(tc::smem_u32(hf == QK_PARTS - 1 ? &s_full[w] : &s_half[w]));
-          }
-          if (W == 1 || w == 1) tc::umma_commit(tc::smem_u32(&k_empty[s]));
-        }
-        if (W == 1 || w == 1) ++kc;
-        return true;
+          if (!ok || !it.next(a)) break;
+          entry = tile_entry(a, it.b, it.kt0);
+        } while (true);
+      }
+    } else if (warp == 1) {
+      // -------------------------------------------------------------------- MMA issuer (one elected lane), query tiles
+      const bool leader = tc::elect_one();
+      constexpr int QK_PARTS = FP8 ? 1 : 2;       // (FP8: shared-memory bandwidth counts, and each part reads Q again)
+      constexpr uint32_t idesc_qk = tc::umma_idesc(128, TT_KEYS / QK_PARTS, 0, 0, MMA_F16, MMA_F16);
+      constexpr uint32_t idesc_pv = tc::umma_idesc(128, HD, 0, 1, MMA_F16, MMA_F16);
+      const uint64_t q_desc = tc::umma_desc_sw128(tc::smem_u32(smem + L::Q), 16, 1024);
+      const uint64_t k_desc = tc::umma_desc_sw128(tc::smem_u32(smem + L::K), 16, 1024);
+      const uint64_t v_desc = tc::umma_desc_sw128(tc::smem_u32(smem + L::V), L::CHUNK, 1024);
+      int kc = 0, vc = 0, item = 0, sc0 = 0, sc1 = 0;
+      bool ok = true, more;
+      auto load_q = [&]() {
+        const uint32_t bar = tc::smem_u32(q_full);
+        const int copies = FP8 ? p.copies : 1;
+        tc::mbar_expect_tx(bar, W * copies * L::CHUNKS * p.npt * rep * 128);
+        for (int w = 0; w < W; ++w)
+          for (int q = 0; q < copies; ++q)
+            for (int c = 0; c < L::CHUNKS; ++c)
+              tc::tma_load_3d(tc::smem_u32(smem + L::Q + w * L::TILE + c * L::CHUNK + q * (128 / copies) * 128), &tmQ, bar, c * 64, it.h * rep,
+                              it.s.tok0 + (it.g * W + w) * p.npt);
       };
-      ok = wait(FP8 ? q_ready : q_full, item & 1);
-      tc::tc_fence_after_sync();
-      ok = ok && issue_qk(0);
-      for (int step = 0; step < steps && ok; ++step) {
-        if (step + 1 < steps && !(ok = issue_qk(step + 1))) break;
-        const int w = step & 1, s = vc % L::VS;
-        if (W == 1 || w == 0)
-          if (!(ok = wait(&v_full[s], (vc / L::VS) & 1))) break;
-        if (step == 0 && !(ok = wait(o_empty, (item & 1) ^ 1))) break;
-        // O += P V in two halves of 64 keys, in the order in which the softmax warps finish them
-        constexpr int FIRST = FP8 ? 0 : 1;
-        int &sc = w ? sc1 : sc0;
-        const uint64_t vd = v_desc + (uint64_t)(s * (L::TILE >> 4));
-        auto issue_pv = [&](int hf, bool accumulate) {
+      if (leader) load_q();
+      do {
+        const int nt = it.kt1 - it.kt0, steps = W == 2 ? 2 * nt : nt;
+        // S of a step; steps alternate between the streams.  The stream's last P V was issued before, and runs before.
+        auto issue_qk = [&](int step) -> bool {
+          const int w = step & 1, s = kc % L::KS;
+          if (W == 1 || w == 0) {
+            if (!wait(&k_full[s], (kc / L::KS) & 1)) return false;
+            tc::tc_fence_after_sync();
+          }
+          if (leader) {
+            // the scores of 64 keys after the other 64: the softmax warps start on the first half
+            const uint64_t qd = q_desc + (uint64_t)((W == 2 ? w : 0) * (L::TILE >> 4)), kd = k_desc + (uint64_t)(s * (L::TILE >> 4));
 #pragma unroll
-          for (int k4 = 0; k4 < TT_KEYS / 32; ++k4)
-            tc::umma_ts(tmem_base + 256 + w * 128, tmem_base + w * 128 + hf * 64 + k4 * 8, vd + (uint64_t)(((hf * 4 + k4) * 16 * 128) >> 4), idesc_pv,
-                        (accumulate || k4 != 0) ? 1u : 0u);
+            for (int hf = 0; hf < QK_PARTS; ++hf) {
+#pragma unroll
+              for (int kk = 0; kk < HD / 16; ++kk) {
+                const uint32_t off = ((kk >> 2) * L::CHUNK + (kk & 3) * 32) >> 4;
+                tc::umma_ss(tmem_base + w * 128 + hf * 64, qd + off, kd + off + hf * (64 * 128 >> 4), idesc_qk, kk != 0);
+              }
+              tc::umma_commit(tc::smem_u32(hf == QK_PARTS - 1 ? &s_full[w] : &s_half[w]));
+            }
+            if (W == 1 || w == 1) tc::umma_commit(tc::smem_u32(&k_empty[s]));
+          }
+          if (W == 1 || w == 1) ++kc;
+          return true;
         };
-        if (!(ok = wait(&p_part[FIRST * 2 + w], sc & 1))) break;
+        ok = wait(FP8 ? q_ready : q_full, item & 1);
         tc::tc_fence_after_sync();
-        if (leader) issue_pv(FIRST, step > 1);
-        if (!(ok = wait(&p_part[(1 - FIRST) * 2 + w], sc & 1))) break;
-        ++sc;
-        tc::tc_fence_after_sync();
-        if (leader) {
-          issue_pv(1 - FIRST, true);
-          if (W == 1 || w == 1) tc::umma_commit(tc::smem_u32(&v_empty[s]));
-          if (step == steps - 1) tc::umma_commit(tc::smem_u32(o_full));
-        }
-        if (W == 1 || w == 1) ++vc;
-      }
-      ++item;
-      __syncwarp();
-      // the next piece's queries: every Q K^T of this one has retired (its last P came from it), so their place is free
-      more = ok && it.next(a);
-      if (more && leader) load_q();
-    } while (more);
-  } else if (FP8 && warp == 2) {
-    // -------------------------------------------------------------------- row scales, four keys per lane, a tile ahead of their use
-    int tile = 0;
-    bool ok = true;
-    do {
-      const int kv_len = it.s.past + it.s.n;
-      float k1[4], v1[4], k0[4], v0[4];
-      auto request = [&](int entry, int j, float (&k)[4], float (&v)[4]) {
-        const int base = tile_row(a, entry, j);
+        ok = ok && issue_qk(0);
+        for (int step = 0; step < steps && ok; ++step) {
+          if (step + 1 < steps && !(ok = issue_qk(step + 1))) break;
+          const int w = step & 1, s = vc % L::VS;
+          if (W == 1 || w == 0)
+            if (!(ok = wait(&v_full[s], (vc / L::VS) & 1))) break;
+          if (step == 0 && !(ok = wait(o_empty, (item & 1) ^ 1))) break;
+          // O += P V in two halves of 64 keys, in the order in which the softmax warps finish them
+          constexpr int FIRST = FP8 ? 0 : 1;
+          int &sc = w ? sc1 : sc0;
+          const uint64_t vd = v_desc + (uint64_t)(s * (L::TILE >> 4));
+          auto issue_pv = [&](int hf, bool accumulate) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int key = i * 32 + lane, row = base + key;
-          const bool there = j < it.kt1 && j * TT_KEYS + key < kv_len && row >= 0 && row < a.cache_rows;
-          k[i] = there ? a.k_scale[row] : 0.f;
-          v[i] = there ? a.v_scale[row] : 0.f;
+            for (int k4 = 0; k4 < TT_KEYS / 32; ++k4)
+              tc::umma_ts(tmem_base + 256 + w * 128, tmem_base + w * 128 + hf * 64 + k4 * 8, vd + (uint64_t)(((hf * 4 + k4) * 16 * 128) >> 4), idesc_pv,
+                          (accumulate || k4 != 0) ? 1u : 0u);
+          };
+          if (!(ok = wait(&p_part[FIRST * 2 + w], sc & 1))) break;
+          tc::tc_fence_after_sync();
+          if (leader) issue_pv(FIRST, step > 1);
+          if (!(ok = wait(&p_part[(1 - FIRST) * 2 + w], sc & 1))) break;
+          ++sc;
+          tc::tc_fence_after_sync();
+          if (leader) {
+            issue_pv(1 - FIRST, true);
+            if (W == 1 || w == 1) tc::umma_commit(tc::smem_u32(&v_empty[s]));
+            if (step == steps - 1) tc::umma_commit(tc::smem_u32(o_full));
+          }
+          if (W == 1 || w == 1) ++vc;
         }
-      };
-      int entry1 = tile_entry(a, it.b, min(it.kt0 + 1, it.kt1 - 1));
-      request(tile_entry(a, it.b, it.kt0), it.kt0, k1, v1);
-      for (int j = it.kt0; j < it.kt1 && ok; ++j, ++tile) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { k0[i] = k1[i]; v0[i] = v1[i]; }
-        request(entry1, j + 1, k1, v1);
-        entry1 = tile_entry(a, it.b, min(j + 2, it.kt1 - 1));
-        if (!(ok = wait(&g_empty[tile & 3], ((tile >> 2) & 1) ^ 1))) break;
-        float *to = scales + (tile & 3) * 384;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          to[i * 32 + lane] = k0[i];
-          to[128 + i * 32 + lane] = v0[i];
-          to[256 + i * 32 + lane] = fminf(fmaxf(__log2f(v0[i]), -126.f), 60.f);      // (beyond 2^60 P itself overflows)
-        }
+        ++item;
         __syncwarp();
-        if (lane == 0) tc::mbar_arrive(tc::smem_u32(&g_full[tile & 3]));
-      }
-    } while (ok && it.next(a));
-  }
+        // the next piece's queries: every Q K^T of this one has retired (its last P came from it), so their place is free
+        more = ok && it.next(a);
+        if (more && leader) load_q();
+      } while (more);
+    } else if (FP8 && warp == 2) {
+      // -------------------------------------------------------------------- row scales, four keys per lane, a tile ahead of their use
+      int tile = 0;
+      bool ok = true;
+      do {
+        const int kv_len = it.s.past + it.s.n;
+        float k1[4], v1[4], k0[4], v0[4];
+        auto request = [&](int entry, int j, float (&k)[4], float (&v)[4]) {
+          const int base = tile_row(a, entry, j);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int key = i * 32 + lane, row = base + key;
+            const bool there = j < it.kt1 && j * TT_KEYS + key < kv_len && row >= 0 && row < a.cache_rows;
+            k[i] = there ? a.k_scale[row] : 0.f;
+            v[i] = there ? a.v_scale[row] : 0.f;
+          }
+        };
+        int entry1 = tile_entry(a, it.b, min(it.kt0 + 1, it.kt1 - 1));
+        request(tile_entry(a, it.b, it.kt0), it.kt0, k1, v1);
+        for (int j = it.kt0; j < it.kt1 && ok; ++j, ++tile) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) { k0[i] = k1[i]; v0[i] = v1[i]; }
+          request(entry1, j + 1, k1, v1);
+          entry1 = tile_entry(a, it.b, min(j + 2, it.kt1 - 1));
+          if (!(ok = wait(&g_empty[tile & 3], ((tile >> 2) & 1) ^ 1))) break;
+          float *to = scales + (tile & 3) * 384;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            to[i * 32 + lane] = k0[i];
+            to[128 + i * 32 + lane] = v0[i];
+            to[256 + i * 32 + lane] = fminf(fmaxf(__log2f(v0[i]), -126.f), 60.f);      // (beyond 2^60 P itself overflows)
+          }
+          __syncwarp();
+          if (lane == 0) tc::mbar_arrive(tc::smem_u32(&g_full[tile & 3]));
+        }
+      } while (ok && it.next(a));
+    }
   } else if (warp < L::SOFT + 8) {
     if constexpr (FP8) asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
     // -------------------------------------------------------------------- softmax: stream w, a query row per thread
@@ -700,35 +705,33 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
         const bool edge = j0 > -TT_KEYS;                              // holds new tokens (and perhaps rows behind them)
         if (!(ok = wait(FP8 ? &s_full[w] : &s_half[w], sc & 1))) break;
         tc::tc_fence_after_sync();
-        {
-          if (edge && (W == 1 || w == 0)) {
-            // V rows that must not meet a zero probability as NaN or infinity (comment at the top).  Behind the wait for S: it was issued
-            // after the P V of two tiles before, so the V ring's place is in this tile's phase or the one before, never two before,
-            // which the parity could not tell from this one.
-            const int s = tile % L::VS, key = j0 + r;
-            if (!(ok = wait(&v_full[s], (tile / L::VS) & 1))) break;
-            if (key >= 0) {
-              uint8_t *vrow = smem + L::V + s * L::TILE + r * 128;
-              const bool behind = key >= it.s.n;
-              bool handed = false;
-              constexpr uint32_t e = MMA_F16 ? 0x7c007c00u : 0x7f807f80u;
+        if (edge && (W == 1 || w == 0)) {
+          // V rows that must not meet a zero probability as NaN or infinity (comment at the top).  Behind the wait for S: it was issued
+          // after the P V of two tiles before, so the V ring's place is in this tile's phase or the one before, never two before,
+          // which the parity could not tell from this one.
+          const int s = tile % L::VS, key = j0 + r;
+          if (!(ok = wait(&v_full[s], (tile / L::VS) & 1))) break;
+          if (key >= 0) {
+            uint8_t *vrow = smem + L::V + s * L::TILE + r * 128;
+            const bool behind = key >= it.s.n;
+            bool handed = false;
+            constexpr uint32_t e = MMA_F16 ? 0x7c007c00u : 0x7f807f80u;
 #pragma unroll 1
-              for (int i = 0; i < L::CHUNKS * 8; ++i) {
-                uint4 *at = reinterpret_cast<uint4 *>(vrow + (i >> 3) * L::CHUNK + (i & 7) * 16);
-                const uint4 x = *at;
-                uint32_t xs[4] = {x.x, x.y, x.z, x.w}, worst = 0;
+            for (int i = 0; i < L::CHUNKS * 8; ++i) {
+              uint4 *at = reinterpret_cast<uint4 *>(vrow + (i >> 3) * L::CHUNK + (i & 7) * 16);
+              const uint4 x = *at;
+              uint32_t xs[4] = {x.x, x.y, x.z, x.w}, worst = 0;
 #pragma unroll
-                for (int q4 = 0; q4 < 4; ++q4) {
-                  const uint32_t gone = ((xs[q4] & e & 0xffff0000u) == (e & 0xffff0000u) ? 0xffff0000u : 0u) | ((xs[q4] & e & 0xffffu) == (e & 0xffffu) ? 0xffffu : 0u);
-                  worst |= gone;
-                  xs[q4] &= ~gone;
-                }
-                if (behind) *at = make_uint4(0u, 0u, 0u, 0u);
-                else if (worst) { *at = make_uint4(xs[0], xs[1], xs[2], xs[3]); handed = true; }
+              for (int q4 = 0; q4 < 4; ++q4) {
+                const uint32_t gone = ((xs[q4] & e & 0xffff0000u) == (e & 0xffff0000u) ? 0xffff0000u : 0u) | ((xs[q4] & e & 0xffffu) == (e & 0xffffu) ? 0xffffu : 0u);
+                worst |= gone;
+                xs[q4] &= ~gone;
               }
-              if (handed) bad_item[item & 1] = item + 1;
-              if (behind || handed) tc::fence_proxy_async_smem();
+              if (behind) *at = make_uint4(0u, 0u, 0u, 0u);
+              else if (worst) { *at = make_uint4(xs[0], xs[1], xs[2], xs[3]); handed = true; }
             }
+            if (handed) bad_item[item & 1] = item + 1;
+            if (behind || handed) tc::fence_proxy_async_smem();
           }
         }
         const float4 *ksc = reinterpret_cast<const float4 *>(scales + (tile & 3) * 384), *vsc = ksc + 32, *lvs = ksc + 64;
@@ -1292,7 +1295,7 @@ int32_t launch_tc_for(const TreeArgs &a, bool fp8, int max_kv, cudaStream_t st) 
   TreeTcArgs p{};
   p.a = a;
   const int rep = a.n_q / a.n_kv;
-  // (24 sequences of 10000 keys, 32 rows: 187 us in four copies, 210 us in two, 283 us in one; 64 rows: 219 us in two, 286 us in one)
+  // (24 sequences of 10000 keys, 32 rows: 170 us in four copies, 214 us in two, 294 us in one; 64 rows: 222 us in two, 300 us in one)
   p.copies = !fp8 ? 1 : a.max_new * rep <= 32 ? 4 : a.max_new * rep <= 64 ? 2 : 1;
   while (p.copies > 1 && (long long)p.copies * a.total_new > TC_COPY_TOKENS) p.copies /= 2;
   p.npt = 128 / p.copies / rep;
