@@ -257,7 +257,7 @@ size_t simt_scratch(int total_new, int max_kv, int n_q, int hd) {
 // What bounds it: HBM for 16-bit caches and up to about 64 query rows per KV head (24 sequences of one token over 10000 keys 158 us,
 // 0.96 of the copy bandwidth; 16 of 9 to 32 tokens over 2048 to 8192 keys 70 us, 4.3 TB/s); each stream's chain of softmax, P V and next
 // Q K^T for two full tiles (2 x 64 tokens, 8 heads per KV head, over 131072 keys 470 - 520 us, 1.0 - 1.1 PFLOP/s); shared memory for FP8
-// caches (24 sequences of up to 8 tokens over up to 10000 keys 145 us, 2.5 TB/s); latency for few keys (1 token over 700 keys 12 us).
+// caches (24 sequences of up to 8 tokens over up to 10000 keys 143 us, 2.5 TB/s); latency for few keys (1 token over 700 keys 12 us).
 //
 // What is not seen must not matter: keys behind the sequence and unseen drafts get S = -inf, and the V rows of the last
 // tiles are cleaned in shared memory first (0 * NaN is NaN): rows behind the sequence become zeros, and so do infinities and NaN in a
@@ -718,7 +718,7 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
             constexpr uint32_t e = MMA_F16 ? 0x7c007c00u : 0x7f807f80u;
 #pragma unroll 1
             for (int i = 0; i < L::CHUNKS * 8; ++i) {
-              uint4 *at = reinterpret_cast<uint4 *>(vrow + (i >> 3) * L::CHUNK + (i & 7) * 16);
+              uint4 *at = reinterpret_cast<uint4 *>(vrow + (i >> 3) * L::CHUNK + ((i ^ r) & 7) * 16);      // (eight rows, eight bank groups)
               const uint4 x = *at;
               uint32_t xs[4] = {x.x, x.y, x.z, x.w}, worst = 0;
 #pragma unroll
@@ -1044,11 +1044,11 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
       if (!(ok = wait(q_full, item & 1))) break;
       float back = 1.f;
       if constexpr (!F16) {
-        uint8_t *qrow = smem + L::Q + t * 128;
+        uint8_t *qrow = smem + L::Q + t * 128;               // (its pieces in an order that has eight lanes in eight bank groups)
         uint32_t top = 0;
 #pragma unroll 1
         for (int i = 0; i < L::CHUNKS * 8; ++i) {
-          const uint4 x = *reinterpret_cast<const uint4 *>(qrow + (i >> 3) * L::CHUNK + (i & 7) * 16);
+          const uint4 x = *reinterpret_cast<const uint4 *>(qrow + (i >> 3) * L::CHUNK + ((i ^ t) & 7) * 16);
           const uint32_t xs[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
           for (int q4 = 0; q4 < 4; ++q4) top = max(top, max(xs[q4] & 0x7f80u, (xs[q4] >> 16) & 0x7f80u));
@@ -1060,7 +1060,7 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
         back = __uint_as_float((uint32_t)(127 - shift) << 23);
 #pragma unroll 1
         for (int i = 0; i < L::CHUNKS * 8; ++i) {
-          uint4 *at = reinterpret_cast<uint4 *>(qrow + (i >> 3) * L::CHUNK + (i & 7) * 16);
+          uint4 *at = reinterpret_cast<uint4 *>(qrow + (i >> 3) * L::CHUNK + ((i ^ t) & 7) * 16);
           const uint4 x = *at;
           uint32_t xs[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
