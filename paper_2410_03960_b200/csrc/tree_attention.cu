@@ -257,7 +257,7 @@ size_t simt_scratch(int total_new, int max_kv, int n_q, int hd) {
 // What bounds it: HBM for 16-bit caches and up to about 64 query rows per KV head (24 sequences of one token over 10000 keys 158 us,
 // 0.96 of the copy bandwidth; 16 of 9 to 32 tokens over 2048 to 8192 keys 70 us, 4.3 TB/s); each stream's chain of softmax, P V and next
 // Q K^T for two full tiles (2 x 64 tokens, 8 heads per KV head, over 131072 keys 470 - 520 us, 1.0 - 1.1 PFLOP/s); shared memory for FP8
-// caches (24 sequences of up to 8 tokens over up to 10000 keys 143 us, 2.5 TB/s); latency for few keys (1 token over 700 keys 12 us).
+// caches (24 sequences of up to 8 tokens over up to 10000 keys 130 us, 2.8 TB/s); latency for few keys (1 token over 700 keys 11.9 us).
 //
 // What is not seen must not matter: keys behind the sequence and unseen drafts get S = -inf, and the V rows of the last
 // tiles are cleaned in shared memory first (0 * NaN is NaN): rows behind the sequence become zeros, and so do infinities and NaN in a
@@ -1125,7 +1125,8 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
   }
 }
 
-// joins the partial results of the pieces that a (sequence, group, head) was cut into: block per new token and TJ_THREADS / (HD / 4) heads
+// joins the partial results of the pieces that a (sequence, group, head) was cut into: gridDim.y blocks per new token, TJ_THREADS / (HD / 4) heads
+// at a time
 constexpr int TJ_THREADS = 256;
 template <int HD, bool F16>
 __global__ void __launch_bounds__(TJ_THREADS) tree_attention_tc_join_kernel(TreeTcArgs p, int grid, int tiles_per_group) {
@@ -1149,7 +1150,8 @@ __global__ void __launch_bounds__(TJ_THREADS) tree_attention_tc_join_kernel(Tree
     }
   }
 #pragma unroll
-  for (int k = 0; k < 2; ++k)
+  for (int k = 0; k < 2; ++k) {
+    if (k >= p.classes) break;
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
       int v = sum[k][q];
@@ -1157,84 +1159,96 @@ __global__ void __launch_bounds__(TJ_THREADS) tree_attention_tc_join_kernel(Tree
       for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
       if (lane == 0) s_sum[k][q][warp] = v;
     }
+  }
   __syncthreads();
   wait_for_previous();
   const int b = s_b;
   if (b < 0) return;                                       // a row behind the last sequence
-  constexpr int LANES = HD / 4, PER_PASS = TJ_THREADS / LANES;
-  const int d = (tid % LANES) * 4, hq = blockIdx.y * PER_PASS + tid / LANES, h = hq / rep;
-  if (hq >= a.n_q) return;
-  // the CTAs that worked on this row's item, of one class, in the order of the keys
-  int cls = 0, c0 = 0, n = 0, row = 0;
+  // what the classes do of this token's sequence
+  SeqShape of[2];
+  int before[2] = {0, 0}, per[2] = {1, 1};
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     if (k >= p.classes) break;
-    const SeqShape s = seq_shape(a, b, Split{group_tokens, p.classes, k});
-    const int node = t - s.tok0, g = node / group_tokens;
-    if (g < s.g0 || g >= s.g0 + s.groups || (h - s.h0) % s.h_step) continue;
-    int before = 0, total = 0;
+    of[k] = seq_shape(a, b, Split{group_tokens, p.classes, k});
+    int total = 0;
 #pragma unroll
-    for (int w = 0; w < TJ_THREADS / 32; ++w) { before += s_sum[k][0][w]; total += s_sum[k][1][w]; }
-    const int ctas = (grid - k + p.classes - 1) / p.classes, per = (total + ctas - 1) / ctas;
-    const int first = before + ((g - s.g0) * s.heads + (h - s.h0) / s.h_step) * s.tiles;
-    cls = k;
-    row = (node - g * group_tokens) * rep + hq % rep;
-    c0 = first / per;
-    n = (first + s.tiles - 1) / per - c0 + 1;
+    for (int w = 0; w < TJ_THREADS / 32; ++w) { before[k] += s_sum[k][0][w]; total += s_sum[k][1][w]; }
+    const int ctas = (grid - k + p.classes - 1) / p.classes;
+    per[k] = max(1, (total + ctas - 1) / ctas);
   }
-  const int pieces = n;
-  n *= p.copies;
-  if (n <= 1) return;                                      // whole: already in `out`
-  // the first piece starts at the first key: its CTA's slot 1; the others are the first piece of theirs: slot 0.  Copies of a complete
-  // piece (a CTA may have many of these): by token and head.
-  auto piece = [&](int ic) -> size_t {
-    const int i = ic / p.copies, copy = ic % p.copies;
-    if (pieces == 1) return (size_t)grid * 2 * p.slot_rows + ((size_t)copy * a.total_new + t) * a.n_q + hq;
-    return (size_t)(((c0 + i) * p.classes + cls) * 2 + (i == 0 ? 1 : 0)) * p.slot_rows + copy * (128 / p.copies) + row;
-  };
-  const float2 *ml = reinterpret_cast<const float2 *>(a.scratch);
-  float m = -INFINITY, l = 0.f, o0 = 0.f, o1 = 0.f, o2 = 0.f, o3 = 0.f;
-  for (int i0 = 0; i0 < n; i0 += 4) {                      // four pieces in flight
-    float2 x[4];
-    float4 u[4];
+  const int node = t - of[0].tok0, g = node / group_tokens;
+  constexpr int LANES = HD / 4, PER_PASS = TJ_THREADS / LANES;
+  const int d = (tid % LANES) * 4, shift = p.copies == 4 ? 2 : p.copies == 2 ? 1 : 0;
+#pragma unroll 1
+  for (int hq = blockIdx.y * PER_PASS + tid / LANES; hq < a.n_q; hq += gridDim.y * PER_PASS) {
+    // the CTAs that worked on this row's item, of one class, in the order of the keys
+    const int h = hq / rep, row = (node - g * group_tokens) * rep + hq % rep;
+    int cls = 0, c0 = 0, n = 0;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      x[q] = make_float2(-INFINITY, 0.f);
-      if (i0 + q < n) {
-        const size_t at = piece(i0 + q);
-        x[q] = ml[at];
-        u[q] = *reinterpret_cast<const float4 *>(p.part_o + at * HD + d);
+    for (int k = 0; k < 2; ++k) {
+      if (k >= p.classes) break;
+      const SeqShape &s = of[k];
+      if (g < s.g0 || g >= s.g0 + s.groups || (h - s.h0) % s.h_step) continue;
+      const int first = before[k] + ((g - s.g0) * s.heads + (h - s.h0) / s.h_step) * s.tiles;
+      cls = k;
+      c0 = first / per[k];
+      n = (first + s.tiles - 1) / per[k] - c0 + 1;
+    }
+    const int pieces = n;
+    n *= p.copies;
+    if (n <= 1) continue;                                    // whole: already in `out`
+    // the first piece starts at the first key: its CTA's slot 1; the others are the first piece of theirs: slot 0.  Copies of a complete
+    // piece (a CTA may have many of these): by token and head.
+    auto piece = [&](int ic) -> size_t {
+      const int i = ic >> shift, copy = ic & (p.copies - 1);
+      if (pieces == 1) return (size_t)grid * 2 * p.slot_rows + ((size_t)copy * a.total_new + t) * a.n_q + hq;
+      return (size_t)(((c0 + i) * p.classes + cls) * 2 + (i == 0 ? 1 : 0)) * p.slot_rows + copy * (128 >> shift) + row;
+    };
+    const float2 *ml = reinterpret_cast<const float2 *>(a.scratch);
+    float m = -INFINITY, l = 0.f, o0 = 0.f, o1 = 0.f, o2 = 0.f, o3 = 0.f;
+    for (int i0 = 0; i0 < n; i0 += 4) {                      // four pieces in flight
+      float2 x[4];
+      float4 u[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        x[q] = make_float2(-INFINITY, 0.f);
+        if (i0 + q < n) {
+          const size_t at = piece(i0 + q);
+          x[q] = ml[at];
+          u[q] = *reinterpret_cast<const float4 *>(p.part_o + at * HD + d);
+        }
+      }
+      float m_new = m;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) m_new = fmaxf(m_new, x[q].x);
+      const float back = m == -INFINITY ? 0.f : tt_exp2(m - m_new);
+      l *= back; o0 *= back; o1 *= back; o2 *= back; o3 *= back;
+      m = m_new;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const float f = x[q].x == -INFINITY ? 0.f : tt_exp2(x[q].x - m);
+        if (f == 0.f && x[q].y == 0.f) continue;             // saw nothing
+        l = fmaf(x[q].y, f, l);
+        o0 = fmaf(u[q].x, f, o0); o1 = fmaf(u[q].y, f, o1); o2 = fmaf(u[q].z, f, o2); o3 = fmaf(u[q].w, f, o3);
       }
     }
-    float m_new = m;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) m_new = fmaxf(m_new, x[q].x);
-    const float back = m == -INFINITY ? 0.f : tt_exp2(m - m_new);
-    l *= back; o0 *= back; o1 *= back; o2 *= back; o3 *= back;
-    m = m_new;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const float f = x[q].x == -INFINITY ? 0.f : tt_exp2(x[q].x - m);
-      if (f == 0.f && x[q].y == 0.f) continue;             // saw nothing
-      l = fmaf(x[q].y, f, l);
-      o0 = fmaf(u[q].x, f, o0); o1 = fmaf(u[q].y, f, o1); o2 = fmaf(u[q].z, f, o2); o3 = fmaf(u[q].w, f, o3);
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    if (l == 0.f) o0 = o1 = o2 = o3 = 0.f;
+    const size_t head = (size_t)t * a.n_q + hq;
+    uint16_t y[4];
+    if constexpr (F16) {
+      y[0] = __half_as_ushort(__float2half_rn(o0 * inv)); y[1] = __half_as_ushort(__float2half_rn(o1 * inv));
+      y[2] = __half_as_ushort(__float2half_rn(o2 * inv)); y[3] = __half_as_ushort(__float2half_rn(o3 * inv));
+    } else {
+      y[0] = __bfloat16_as_ushort(__float2bfloat16_rn(o0 * inv)); y[1] = __bfloat16_as_ushort(__float2bfloat16_rn(o1 * inv));
+      y[2] = __bfloat16_as_ushort(__float2bfloat16_rn(o2 * inv)); y[3] = __bfloat16_as_ushort(__float2bfloat16_rn(o3 * inv));
     }
+    uint16_t *dst = reinterpret_cast<uint16_t *>(a.out) + head * HD + d;
+    if (p.store32) *reinterpret_cast<uint2 *>(dst) = make_uint2((uint32_t)y[0] | (uint32_t)y[1] << 16, (uint32_t)y[2] | (uint32_t)y[3] << 16);
+    else { dst[0] = y[0]; dst[1] = y[1]; dst[2] = y[2]; dst[3] = y[3]; }
+    if (a.lse && d == 0) a.lse[head] = l == 0.f ? -INFINITY : m * 0.6931471805599453f + logf(l);
   }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  if (l == 0.f) o0 = o1 = o2 = o3 = 0.f;
-  const size_t head = (size_t)t * a.n_q + hq;
-  uint16_t y[4];
-  if constexpr (F16) {
-    y[0] = __half_as_ushort(__float2half_rn(o0 * inv)); y[1] = __half_as_ushort(__float2half_rn(o1 * inv));
-    y[2] = __half_as_ushort(__float2half_rn(o2 * inv)); y[3] = __half_as_ushort(__float2half_rn(o3 * inv));
-  } else {
-    y[0] = __bfloat16_as_ushort(__float2bfloat16_rn(o0 * inv)); y[1] = __bfloat16_as_ushort(__float2bfloat16_rn(o1 * inv));
-    y[2] = __bfloat16_as_ushort(__float2bfloat16_rn(o2 * inv)); y[3] = __bfloat16_as_ushort(__float2bfloat16_rn(o3 * inv));
-  }
-  uint16_t *dst = reinterpret_cast<uint16_t *>(a.out) + head * HD + d;
-  if (p.store32) *reinterpret_cast<uint2 *>(dst) = make_uint2((uint32_t)y[0] | (uint32_t)y[1] << 16, (uint32_t)y[2] | (uint32_t)y[3] << 16);
-  else { dst[0] = y[0]; dst[1] = y[1]; dst[2] = y[2]; dst[3] = y[3]; }
-  if (a.lse && d == 0) a.lse[head] = l == 0.f ? -INFINITY : m * 0.6931471805599453f + logf(l);
 }
 
 // rows of a partial result: those of a group of query tiles, or all that a call has for one KV head
@@ -1285,7 +1299,10 @@ int32_t launch_tc(TreeTcArgs p, int max_kv, cudaStream_t st) {
   cudaError_t e = cudaGetLastError();
   if (e == cudaSuccess && (grid > 1 || p.copies > 1)) {
     constexpr int PER_PASS = TJ_THREADS / (HD / 4);
-    e = launch_early(tree_attention_tc_join_kernel<HD, F16>, dim3(a.total_new, (a.n_q + PER_PASS - 1) / PER_PASS), TJ_THREADS, st, p, grid, W);
+    // few tokens: their heads side by side; many: one block walks over a token's heads, for finding its pieces costs more than joining them
+    // (64 sequences of 32 tokens over 1024 keys: 97 us -> 86; 16 of up to 32 tokens, with one block a token: 69.5 -> 70.8)
+    const int passes = (a.n_q + PER_PASS - 1) / PER_PASS, wide = 8 * num_sms() / a.total_new + 1;
+    e = launch_early(tree_attention_tc_join_kernel<HD, F16>, dim3(a.total_new, passes < wide ? passes : wide), TJ_THREADS, st, p, grid, W);
   }
   return e == cudaSuccess ? SWIFTKV_OK : report_error(SWIFTKV_ERR_CUDA, cudaGetErrorString(e));
 }
