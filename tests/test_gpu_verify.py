@@ -181,6 +181,12 @@ def test_qk_norm_rope_into_an_fp8_cache(T, n_q, n_kv, hd, dt):
         assert (codes[left] == 0x11).all() and (scales[left] == 5).all()
 
 
+@pytest.mark.parametrize("n_kv,hd", [(1, 64), (3, 64), (5, 128), (7, 256), (16, 256), (17, 256), (31, 128), (32, 128), (33, 128), (64, 64)])
+def test_qk_norm_rope_into_an_fp8_cache_of_other_widths(n_kv, hd):
+    """Rows that do not fill their lanes, that fill a block, and that are too wide for one."""
+    test_qk_norm_rope_into_an_fp8_cache(11, n_kv, n_kv, hd, BF)
+
+
 def test_qk_norm_rope_in_place_and_unaligned():
     """q_out = q, keys and values "stored" to plain tensors, and tensors that start off a 16-byte boundary: the same bits."""
     import paper_2410_03960_b200 as P
@@ -405,6 +411,21 @@ MANY = {"few rows": [(300 + 17 * i, 1 + i % 8) for i in range(40)],
 def test_tree_attention_many_pieces_per_block(lens, heads, kind):
     c = tree_case(len(lens), MANY[lens], *heads, BF, fp8=kind == "fp8")
     check_tree(c, *run_tree(c))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp8", "f32"])
+@pytest.mark.parametrize("max_new", [20, 40, 70, 130, 300])
+def test_tree_attention_promised_more_than_comes(kind, max_new):
+    """max_new and max_kv far above what the lengths say (a server passes its limits), sequences of nothing among them."""
+    import paper_2410_03960_b200 as P
+    c = tree_case(max_new, [(300, 3), (0, 0), (1300, 17), (0, 1), (640, 8), (77, 0)], 16, 4, 128, FF if kind == "f32" else BF, fp8=kind == "fp8")
+    c["max_new"] = max_new
+    keys = c["max_kv"]
+    c["max_kv"] = 40000
+    out, lse = run_tree(c)
+    c["max_kv"] = keys
+    check_tree(c, out, lse)
+    P.op_status()
 
 
 def test_tree_attention_more_tokens_than_copies_are_kept_for():
