@@ -428,6 +428,14 @@ def test_tree_attention_promised_more_than_comes(kind, max_new):
     P.op_status()
 
 
+@pytest.mark.parametrize("kind", ["bf16", "f16", "fp8", "f32"])
+@pytest.mark.parametrize("heads", [(4, 1, 128), (6, 2, 64)], ids=str)
+def test_tree_attention_prompt_chunks(kind, heads):
+    """Chunks of prompts (no mask: causal): many groups of query tiles per sequence, a decode token beside them."""
+    c = tree_case(heads[0], [(1400, 900), (3, 300), (801, 1)], *heads, {"bf16": BF, "f16": HF, "fp8": BF, "f32": FF}[kind], fp8=kind == "fp8", mask=False)
+    check_tree(c, *run_tree(c))
+
+
 def test_tree_attention_more_tokens_than_copies_are_kept_for():
     """An FP8 cache and tiles of few rows, but 700, then 2600 of them."""
     for seqs, new in ((700, 1), (1300, 2)):
