@@ -265,6 +265,9 @@ size_t simt_scratch(int total_new, int max_kv, int n_q, int hd) {
 // ---------------------------------------------------------------------------------------------------------
 constexpr int TT_KEYS = 128;
 constexpr float TT_RESCALE = 8.0f;       // in log2 units
+// FP8: how far a small V scale (0 for a row outside the cache) draws the reference below the scores.  A key adds at most 2^(80 + TT_RESCALE) to the
+// sum, so 2^30 of them stay below 2^127; rows quantized from zeros (2^-64 / 448) lie above.
+constexpr float TT_LEAST_LOG2 = -80.f;
 
 template <int HD, int W, bool FP8>
 struct TreeLayout {
@@ -305,6 +308,12 @@ __device__ __forceinline__ bool tt_wait(uint32_t bar, uint32_t parity, volatile 
       }
     }
   }
+}
+// natural logarithm of l 2^m: with an FP8 cache m and the logarithm of l may be large and cancel
+__device__ __forceinline__ float tt_lse(float m, float l, bool fp8) {
+  if (!fp8 || !(l >= 1.1754944e-38f && l < INFINITY)) return m * 0.6931471805599453f + logf(l);
+  const int bits = __float_as_int(l), e = (bits >> 23) - 127;
+  return (m + (float)e + log2f(__int_as_float((bits & 0x7fffff) | 0x3f800000))) * 0.6931471805599453f;
 }
 __device__ __forceinline__ float tt_exp2(float x) {
   float y;
@@ -670,7 +679,7 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
           for (int i = 0; i < 4; ++i) {
             to[i * 32 + lane] = k0[i];
             to[128 + i * 32 + lane] = v0[i];
-            to[256 + i * 32 + lane] = fminf(fmaxf(__log2f(v0[i]), -126.f), 60.f);      // (beyond 2^60 P itself overflows)
+            to[256 + i * 32 + lane] = fminf(fmaxf(__log2f(v0[i]), TT_LEAST_LOG2), 60.f);      // (beyond 2^60 P itself overflows)
           }
           __syncwarp();
           if (lane == 0) tc::mbar_arrive(tc::smem_u32(&g_full[tile & 3]));
@@ -953,7 +962,7 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
         const int col0 = W == 1 ? w * COLS : 0;
         if (valid && col0 == 0 && (W == 2 || w == 0)) {
           if (!whole) reinterpret_cast<float2 *>(a.scratch)[srow] = make_float2(m * cm, l);
-          else if (a.lse) a.lse[head] = l == 0.f ? -INFINITY : m * (cm * 0.6931471805599453f) + logf(l);
+          else if (a.lse) a.lse[head] = l == 0.f ? -INFINITY : FP8 ? tt_lse(m, l, true) : m * (cm * 0.6931471805599453f) + logf(l);
         }
 #pragma unroll 1
         for (int ch = 0; ch < COLS / 32; ++ch) {
@@ -1247,7 +1256,7 @@ __global__ void __launch_bounds__(TJ_THREADS) tree_attention_tc_join_kernel(Tree
     uint16_t *dst = reinterpret_cast<uint16_t *>(a.out) + head * HD + d;
     if (p.store32) *reinterpret_cast<uint2 *>(dst) = make_uint2((uint32_t)y[0] | (uint32_t)y[1] << 16, (uint32_t)y[2] | (uint32_t)y[3] << 16);
     else { dst[0] = y[0]; dst[1] = y[1]; dst[2] = y[2]; dst[3] = y[3]; }
-    if (a.lse && d == 0) a.lse[head] = l == 0.f ? -INFINITY : m * 0.6931471805599453f + logf(l);
+    if (a.lse && d == 0) a.lse[head] = l == 0.f ? -INFINITY : tt_lse(m, l, a.k_scale != nullptr);
   }
 }
 

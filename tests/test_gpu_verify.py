@@ -607,6 +607,57 @@ def test_tree_attention_reports_lengths_and_pages():
             P.op_status()
 
 
+def rows_gone(c):
+    """The same case for the reference, with the rows outside the cache (-1) as one more row of zeros."""
+    one_more = lambda t: None if t is None else torch.cat([t, torch.zeros_like(t[:1])])  # noqa: E731
+    end = c["k"].shape[0]
+    return dict(c, rows=[np.where(r < 0, end, r) for r in c["rows"]], **{name: one_more(c[name]) for name in ("k", "v", "ks", "vs")})
+
+
+def lose_pages(c, b, pages, entry=-1):
+    for j in pages:
+        c["table"][b, j] = entry
+        c["rows"][b][j * 128: (j + 1) * 128] = -1
+
+
+@pytest.mark.parametrize("kind", ["bf16 fp8", "f16 fp8", "f32 fp8", "bf16"])
+@pytest.mark.parametrize("n", [1, 8, 12, 20])
+@pytest.mark.parametrize("gone", [[0], [3], [5], [0, 5], [0, 1, 2, 3, 4, 5], []], ids=str)
+def test_tree_attention_pages_that_are_missing(kind, n, gone):
+    """Pages outside the cache read as zeros, first, in the middle, last, all of them; a second sequence has none at all.  4 rows per token
+    and KV head: with an FP8 cache a query tile is laid out 4, 4, 2 and 1 times."""
+    import paper_2410_03960_b200 as P
+    c = tree_case(100 + n, [(700, n), (60, n)], 32, 8, 128, {"bf16": BF, "f16": HF, "f32": FF}[kind.split()[0]], fp8="fp8" in kind)
+    lose_pages(c, 0, gone, -1 if n < 12 else 10 ** 6)
+    lose_pages(c, 1, [0])
+    check_tree(rows_gone(c), *run_tree(c))
+    P.op_status()
+
+
+@pytest.mark.parametrize("kind", ["bf16 fp8", "f16 fp8", "bf16"])
+@pytest.mark.parametrize("n", [2, 20])
+def test_tree_attention_pieces_of_missing_pages(kind, n):
+    """Runs of missing pages as long as what a block of the grid works on, so that whole pieces of a sequence hold nothing else."""
+    c = tree_case(130 + n, [(9000, n)], 32, 8, 128, HF if "f16" in kind.split() else BF, fp8="fp8" in kind)
+    lose_pages(c, 0, list(range(0, 9)) + list(range(30, 44)) + [69, 70])
+    check_tree(rows_gone(c), *run_tree(c))
+
+
+@pytest.mark.parametrize("n", [1, 12, 20])
+@pytest.mark.parametrize("scale", [0.0, 2.0 ** -64 / 448, 1e-38])
+def test_tree_attention_rows_of_zeros_in_v(n, scale):
+    """FP8 pages whose V rows are zero: by a scale of 0 (or next to it), or quantized from zeros."""
+    for dt in (BF, HF, FF):
+        c = tree_case(140 + n, [(700, n), (60, n), (5000, n)], 16, 4, 128, dt, fp8=True)
+        for b, pages in ((0, (0, 5)), (1, (0,)), (2, range(10, 20))):
+            for j in pages:
+                rows = torch.as_tensor(c["rows"][b][j * 128: (j + 1) * 128], device="cuda")
+                c["vs"][rows] = scale
+                if scale:
+                    c["v"][rows] = 0
+        check_tree(c, *run_tree(c))
+
+
 @pytest.mark.parametrize("kind", ["bf16", "fp8", "f32"])
 @pytest.mark.parametrize("past", [50, 2100])
 def test_tree_attention_rows_cut_off_a_sequence(kind, past):
