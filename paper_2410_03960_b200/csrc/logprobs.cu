@@ -344,11 +344,12 @@ template <typename T, bool TOP>
 __device__ __forceinline__ void lp_write(const LpShared &sh, const LpArgs &a, const LpSums &all, int row, int tgt, float tgt_v) {
   constexpr float LN2 = 0.6931471805599453f;
   const int lane = threadIdx.x & 31, k = a.top_k;
+  // no finite logit, or none beside a NaN of its vector: l is 0 or NaN, and only lse may still be a value (-inf)
   const bool none = all.m == -INFINITY;
-  const float log_l = none ? -INFINITY : __log2f(all.l);
+  const float log_l = none ? __uint_as_float(0x7fffffffu) : __log2f(all.l);
   if (lane == 0) {
     a.lse[row] = none ? -INFINITY + all.l : fmaf(all.m, a.inv_t, log_l * LN2);
-    a.entropy[row] = none ? __uint_as_float(0x7fffffffu) : (log_l - all.s / all.l) * LN2;
+    a.entropy[row] = (log_l - all.s / all.l) * LN2;
     if (tgt >= a.vocab) atomicOr(a.status, STATUS_BAD_TOKEN);
     a.logprob[row] = tgt >= 0 && tgt < a.vocab ? (tgt_v - all.m) * a.inv_t - log_l * LN2 : 0.f;
   }

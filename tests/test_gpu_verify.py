@@ -795,6 +795,27 @@ def test_token_logprobs_masked_and_peaked():
     P.op_status()
 
 
+@pytest.mark.parametrize("dt", [FF, BF, HF])
+@pytest.mark.parametrize("vocab", [3, 4, 8, 9, 5000, 40000])
+def test_token_logprobs_a_nan_in_every_vector(dt, vocab):
+    """Rows of which no thread holds a whole vector without a NaN: finite logits beside it are not the row's maximum, and nothing of the
+    row's results is a number but its top_ids."""
+    import paper_2410_03960_b200 as P
+    rows = 3
+    x = torch.arange(rows * vocab, device="cuda").remainder(11).view(rows, vocab).to(dt)
+    x[0, 2::4] = math.nan                        # one in every 16 bytes of fp32, two of the 16-bit types
+    x[1, 1] = math.nan
+    x[1, 2:] = -math.inf
+    x[2, 0] = math.nan
+    t = i32([0, 0, vocab - 1])
+    k = min(3, vocab)
+    got = P.token_logprobs(x, t, top_k=k)
+    P.op_status()
+    for name in ("lse", "entropy", "logprob", "top_logprobs"):
+        assert torch.isnan(got[name]).all(), (name, got[name])
+    assert got["top_ids"].tolist() == np.argsort(-np.nan_to_num(f64(x), nan=1e30), 1, kind="stable")[:, :k].tolist()
+
+
 def test_token_logprobs_reports_bad_targets():
     import paper_2410_03960_b200 as P
     _, x, t = lp_case(3, 100, BF, 5)
