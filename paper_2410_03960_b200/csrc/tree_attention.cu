@@ -70,10 +70,17 @@ template <> __device__ __forceinline__ __half tree_round<__half>(float v) { retu
 // as fp32 in shared memory.  Scores: a lane per key, a warp per row; output: a thread per element, all rows.
 // ---------------------------------------------------------------------------------------------------------
 constexpr int TS_THREADS = 128, TS_ROWS = 8, TS_KEYS = 32, TS_SPLIT_KEYS = 1024, TS_MAX_SPLITS = 32;
+// At most so many partial rows: 16384 blocks, 110 for each SM, and 68 MB of scratch at head_dim 128.  More query rows than that fill the GPU
+// without splitting the keys.
+constexpr long long TS_PARTS = 131072;
 
-int simt_splits(int max_kv) {
-  const int s = (max_kv + TS_SPLIT_KEYS - 1) / TS_SPLIT_KEYS;
-  return s < 1 ? 1 : s > TS_MAX_SPLITS ? TS_MAX_SPLITS : s;
+long long simt_splits_by_keys(int max_kv) {
+  const long long s = ((long long)max_kv + TS_SPLIT_KEYS - 1) / TS_SPLIT_KEYS;
+  return s < TS_MAX_SPLITS ? s : TS_MAX_SPLITS;
+}
+int simt_splits(int total_new, int max_kv, int n_q) {
+  const long long by_keys = simt_splits_by_keys(max_kv), by_rows = TS_PARTS / ((long long)total_new * n_q);
+  return (int)(by_rows < 1 ? 1 : by_keys < by_rows ? by_keys : by_rows);
 }
 
 template <typename TQ, typename TKV>
@@ -206,7 +213,7 @@ __global__ void __launch_bounds__(TS_THREADS) tree_attention_join_kernel(TreeArg
 
 template <typename TQ, typename TKV>
 int32_t launch_simt(const TreeArgs &a, int max_kv, cudaStream_t st) {
-  const int splits = simt_splits(max_kv), rep = a.n_q / a.n_kv;
+  const int splits = simt_splits(a.total_new, max_kv, a.n_q), rep = a.n_q / a.n_kv;
   const int row_chunks = (a.max_new * rep + TS_ROWS - 1) / TS_ROWS;
   const long long grid = (long long)a.n_seqs * a.n_kv * row_chunks * splits;
   if (grid > 0x7fffffffLL || (long long)a.total_new * a.n_q > 0x7fffffffLL) return report_error(SWIFTKV_ERR_UNSUPPORTED, "too many query rows for one launch");
@@ -222,9 +229,10 @@ int32_t launch_simt(const TreeArgs &a, int max_kv, cudaStream_t st) {
   return e == cudaSuccess ? SWIFTKV_OK : report_error(SWIFTKV_ERR_CUDA, cudaGetErrorString(e));
 }
 
+// (enough for fewer rows and keys as well: these have at most as many partial rows)
 size_t simt_scratch(int total_new, int max_kv, int n_q, int hd) {
-  const int splits = simt_splits(max_kv);
-  return splits > 1 ? (size_t)total_new * n_q * splits * (hd + 2) * sizeof(float) : 0;
+  const long long by_keys = simt_splits_by_keys(max_kv), parts = (long long)total_new * n_q * by_keys;
+  return by_keys > 1 ? (size_t)(parts < TS_PARTS ? parts : TS_PARTS) * (hd + 2) * sizeof(float) : 0;
 }
 
 // ---------------------------------------------------------------------------------------------------------

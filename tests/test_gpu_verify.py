@@ -436,6 +436,15 @@ def test_tree_attention_prompt_chunks(kind, heads):
     check_tree(c, *run_tree(c))
 
 
+def test_tree_attention_many_rows_in_the_general_form():
+    """fp32 rows enough for every SM: the keys are split less often, so that the partial results stay bounded."""
+    import paper_2410_03960_b200 as P
+    for lens, n_q, hd in (([(32700, 300)], 16, 16), ([(2000, 700), (1, 2)], 64, 8)):
+        c = tree_case(len(lens), lens, n_q, 4, hd, FF, mask=False)
+        check_tree(c, *run_tree(c))
+    P.op_status()
+
+
 def test_tree_attention_more_tokens_than_copies_are_kept_for():
     """An FP8 cache and tiles of few rows, but 700, then 2600 of them."""
     for seqs, new in ((700, 1), (1300, 2)):

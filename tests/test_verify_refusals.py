@@ -94,6 +94,17 @@ def test_tree_attention_scratch_grows_with_its_arguments(lib):
             last = now
 
 
+def test_tree_attention_scratch_is_bounded(lib):
+    """A long prompt chunk over a large promised length: partial results of 131072 rows at most, whatever the form, and never less than a
+    smaller call needs."""
+    f = lib.swiftkv_tree_attention_scratch_bytes
+    assert f(16384, 131072, 32, 128) <= 128 << 20 and f(65536, 1 << 20, 64, 256) <= 160 << 20
+    for hd in (32, 128, 256):
+        sizes = [[f(t, kv, 32, hd) for kv in (1, 1024, 1025, 9000, 33000, 1 << 20, 1 << 30)] for t in (1, 2, 60, 128, 129, 300, 4095, 4096, 4097, 50000)]
+        for t, row in enumerate(sizes):
+            assert row == sorted(row) and (t == 0 or all(a <= b for a, b in zip(sizes[t - 1], row)))
+
+
 LP = dict(logits=at(0), stride=1000, dtype=0, targets=at(1), rows=4, vocab=1000, temperature=1.0, top_k=3, logprob=at(2), entropy=at(3), lse=at(4), ids=at(5), top=at(6),
           stream=None)
 
