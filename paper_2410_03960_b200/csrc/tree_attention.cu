@@ -214,13 +214,14 @@ __global__ void __launch_bounds__(TS_THREADS) tree_attention_join_kernel(TreeArg
 template <typename TQ, typename TKV>
 int32_t launch_simt(const TreeArgs &a, int max_kv, cudaStream_t st) {
   const int splits = simt_splits(a.total_new, max_kv, a.n_q), rep = a.n_q / a.n_kv;
-  const int row_chunks = (a.max_new * rep + TS_ROWS - 1) / TS_ROWS;
-  const long long grid = (long long)a.n_seqs * a.n_kv * row_chunks * splits;
-  if (grid > 0x7fffffffLL || (long long)a.total_new * a.n_q > 0x7fffffffLL) return report_error(SWIFTKV_ERR_UNSUPPORTED, "too many query rows for one launch");
+  const long long chunks = ((long long)a.max_new * rep + TS_ROWS - 1) / TS_ROWS;
+  const double blocks = (double)a.n_seqs * a.n_kv * chunks * splits;        // (the products pass 64 bits for the largest arguments)
+  if (blocks > 0x7fffffff || (double)a.total_new * a.n_q > 0x7fffffff) return report_error(SWIFTKV_ERR_UNSUPPORTED, "too many query rows for one launch");
+  const int row_chunks = (int)chunks;
   const size_t smem = ((size_t)TS_ROWS * a.hd + (size_t)TS_KEYS * (2 * a.hd + 1)) * sizeof(float);
   if (smem > 40 * 1024 && ensure_dynamic_smem(reinterpret_cast<const void *>(tree_attention_simt_kernel<TQ, TKV>), 80 * 1024))
     return report_error(SWIFTKV_ERR_CUDA, "shared memory");
-  tree_attention_simt_kernel<TQ, TKV><<<(unsigned)grid, TS_THREADS, smem, st>>>(a, row_chunks, splits);
+  tree_attention_simt_kernel<TQ, TKV><<<(unsigned)blocks, TS_THREADS, smem, st>>>(a, row_chunks, splits);
   cudaError_t e = cudaGetLastError();
   if (e == cudaSuccess && splits > 1) {
     tree_attention_join_kernel<TQ><<<(unsigned)(a.total_new * a.n_q), TS_THREADS, 0, st>>>(a, splits);
@@ -1304,10 +1305,10 @@ int32_t launch_tc(TreeTcArgs p, int max_kv, cudaStream_t st) {
     return report_error(SWIFTKV_ERR_CUDA, "tensor map");
   auto kernel = tree_attention_tc_kernel<HD, W, F16, FP8>;
   if (ensure_dynamic_smem(reinterpret_cast<const void *>(kernel), L::BYTES)) return report_error(SWIFTKV_ERR_CUDA, "shared memory");
-  const long long groups = (a.max_new + W * p.npt - 1) / (W * p.npt), tiles = ((long long)max_kv + TT_KEYS - 1) / TT_KEYS;
-  const long long most = groups * tiles * a.n_kv * a.n_seqs;
-  if (most > 0x7fffffffLL) return report_error(SWIFTKV_ERR_UNSUPPORTED, "too many key tiles for one launch");
-  const int grid = (int)(most < num_sms() ? most : num_sms());
+  const long long groups = ((long long)a.max_new + W * p.npt - 1) / (W * p.npt), tiles = ((long long)max_kv + TT_KEYS - 1) / TT_KEYS;
+  const double most = (double)groups * tiles * a.n_kv * a.n_seqs;
+  if (most > 0x7fffffff) return report_error(SWIFTKV_ERR_UNSUPPORTED, "too many key tiles for one launch");
+  const int grid = most < num_sms() ? (int)most : num_sms();
   p.classes = groups == 2 && grid > 1 ? 2 : 1;
   const size_t rows = (size_t)grid * 2 * p.slot_rows + (p.copies > 1 ? (size_t)p.copies * a.total_new * a.n_q : 0);
   const size_t ml_bytes = (rows * sizeof(float2) + 255) & ~(size_t)255;
@@ -1330,7 +1331,8 @@ int32_t launch_tc_for(const TreeArgs &a, bool fp8, int max_kv, cudaStream_t st) 
   p.a = a;
   const int rep = a.n_q / a.n_kv;
   // (24 sequences of 10000 keys, 32 rows: 170 us in four copies, 214 us in two, 294 us in one; 64 rows: 222 us in two, 300 us in one)
-  p.copies = !fp8 ? 1 : a.max_new * rep <= 32 ? 4 : a.max_new * rep <= 64 ? 2 : 1;
+  const long long rows = (long long)a.max_new * rep;
+  p.copies = !fp8 ? 1 : rows <= 32 ? 4 : rows <= 64 ? 2 : 1;
   while (p.copies > 1 && (long long)p.copies * a.total_new > TC_COPY_TOKENS) p.copies /= 2;
   p.npt = 128 / p.copies / rep;
   p.slot_rows = p.copies > 1 ? 128 : tc_slot_rows(a.total_new, a.n_q, a.n_kv);
@@ -1379,11 +1381,12 @@ extern "C" int32_t swiftkv_tree_attention(const void *q, int64_t q_stride, int32
   if (need && (!scratch || scratch_bytes < need)) return report_error(SWIFTKV_ERR_WORKSPACE_SMALL, "scratch too small (see swiftkv_tree_attention_scratch_bytes)");
   unsigned int *status = op_status_word();
   if (!status) return report_error(SWIFTKV_ERR_CUDA, "no status word");
+  // (max_new: no sequence has more new tokens than there are, so a limit far above them neither picks the kernel's form nor sizes its grid)
   TreeArgs a{};
   a.q = q; a.q_stride = q_stride; a.k = k_cache; a.v = v_cache; a.k_scale = k_scale; a.v_scale = v_scale;
   a.blk = block_table; a.max_blocks = max_blocks; a.row0 = row0; a.past = n_past; a.cu = cu_new; a.mask = tree_mask; a.mask_words = mask_words;
   a.out = out; a.lse = lse; a.scratch = reinterpret_cast<float *>(scratch);
-  a.cache_rows = cache_rows; a.n_seqs = n_seqs; a.total_new = total_new; a.max_new = max_new; a.max_kv = max_kv; a.n_q = n_q_heads; a.n_kv = n_kv_heads; a.hd = head_dim;
+  a.cache_rows = cache_rows; a.n_seqs = n_seqs; a.total_new = total_new; a.max_new = max_new < total_new ? max_new : total_new; a.max_kv = max_kv; a.n_q = n_q_heads; a.n_kv = n_kv_heads; a.hd = head_dim;
   a.scale = softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)head_dim);
   a.status = status;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);

@@ -428,6 +428,30 @@ def test_tree_attention_promised_more_than_comes(kind, max_new):
     P.op_status()
 
 
+@pytest.mark.parametrize("kind", ["bf16", "fp8", "f32"])
+@pytest.mark.parametrize("max_new", [(1 << 29) + 1, 1 << 26, (1 << 31) - 1])
+@pytest.mark.parametrize("heads", [(16, 2, 128), (64, 1, 64)], ids=str)
+def test_tree_attention_promises_of_any_size(kind, max_new, heads):
+    """max_new times the heads of a group beyond 32 bits, and the largest number that there is."""
+    import paper_2410_03960_b200 as P
+    c = tree_case(max_new % 97, [(300, 3), (0, 20), (640, 1)], *heads, FF if kind == "f32" else BF, fp8=kind == "fp8")
+    want, want_lse = run_tree(c)
+    out, lse = run_tree(dict(c, max_new=max_new))
+    check_tree(c, out, lse)
+    assert torch.equal(out, want) and torch.equal(lse, want_lse)
+    P.op_status()
+
+
+def test_tree_attention_limits_of_a_large_server():
+    """256 sequences of one token with limits that no call comes near: the size of the work is the tokens', not the limits'."""
+    import paper_2410_03960_b200 as P
+    c = tree_case(256, [(i, 1) for i in range(256)], 32, 8, 128, BF)
+    keys, c["max_new"], c["max_kv"] = c["max_kv"], 65536, 131072
+    out, lse = run_tree(c)
+    check_tree(dict(c, max_kv=keys), out, lse)
+    P.op_status()
+
+
 @pytest.mark.parametrize("kind", ["bf16", "f16", "fp8", "f32"])
 @pytest.mark.parametrize("heads", [(4, 1, 128), (6, 2, 64)], ids=str)
 def test_tree_attention_prompt_chunks(kind, heads):
