@@ -563,7 +563,7 @@ int32_t swiftkv_qk_norm_rope_bwd(const void *dq, const void *dk, const void *q, 
  *   row0        : int32 [n_seqs] (position p in row row0[b] + p).  A row outside the cache reads as zeros
  *   n_past int32 [n_seqs], cu_new int32 [n_seqs + 1], tree_mask int32 [total_new][mask_words]
  *   max_new, max_kv : at least the largest number of new tokens and of n_past + new tokens of any sequence; a longer sequence is
- *                 cut there and reported
+ *                 cut there (n_past + new tokens at 2^30 in any case) and reported
  *   out         : [total_new][n_q_heads][head_dim] in q_dtype; lse (nullable): fp32 [total_new][n_q_heads], natural logarithm of the
  *                 softmax's denominator.  Rows of tokens that belong to no sequence are left as they were
  *   softmax_scale : 0 means 1/sqrt(head_dim)

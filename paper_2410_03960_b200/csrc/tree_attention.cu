@@ -13,6 +13,8 @@
 namespace skv {
 namespace {
 
+constexpr int TREE_MAX_KV = 1 << 30;      // a longer sequence is cut there
+
 struct TreeArgs {
   const void *q;
   long long q_stride;            // elements between tokens
@@ -212,8 +214,8 @@ __global__ void __launch_bounds__(TS_THREADS) tree_attention_join_kernel(TreeArg
 }
 
 template <typename TQ, typename TKV>
-int32_t launch_simt(const TreeArgs &a, int max_kv, cudaStream_t st) {
-  const int splits = simt_splits(a.total_new, max_kv, a.n_q), rep = a.n_q / a.n_kv;
+int32_t launch_simt(const TreeArgs &a, cudaStream_t st) {
+  const int splits = simt_splits(a.total_new, a.max_kv, a.n_q), rep = a.n_q / a.n_kv;
   const long long chunks = ((long long)a.max_new * rep + TS_ROWS - 1) / TS_ROWS;
   const double blocks = (double)a.n_seqs * a.n_kv * chunks * splits;        // (the products pass 64 bits for the largest arguments)
   if (blocks > 0x7fffffff || (double)a.total_new * a.n_q > 0x7fffffff) return report_error(SWIFTKV_ERR_UNSUPPORTED, "too many query rows for one launch");
@@ -1292,7 +1294,7 @@ bool tc_supported(const TreeArgs &a, bool q16, bool fp8) {
 }
 
 template <int HD, int W, bool F16, bool FP8>
-int32_t launch_tc(TreeTcArgs p, int max_kv, cudaStream_t st) {
+int32_t launch_tc(TreeTcArgs p, cudaStream_t st) {
   using L = TreeLayout<HD, W, FP8>;
   static_assert(L::BYTES <= 232448, "shared memory of one CTA");
   const TreeArgs &a = p.a;
@@ -1305,7 +1307,7 @@ int32_t launch_tc(TreeTcArgs p, int max_kv, cudaStream_t st) {
     return report_error(SWIFTKV_ERR_CUDA, "tensor map");
   auto kernel = tree_attention_tc_kernel<HD, W, F16, FP8>;
   if (ensure_dynamic_smem(reinterpret_cast<const void *>(kernel), L::BYTES)) return report_error(SWIFTKV_ERR_CUDA, "shared memory");
-  const long long groups = ((long long)a.max_new + W * p.npt - 1) / (W * p.npt), tiles = ((long long)max_kv + TT_KEYS - 1) / TT_KEYS;
+  const long long groups = ((long long)a.max_new + W * p.npt - 1) / (W * p.npt), tiles = ((long long)a.max_kv + TT_KEYS - 1) / TT_KEYS;
   const double most = (double)groups * tiles * a.n_kv * a.n_seqs;
   if (most > 0x7fffffff) return report_error(SWIFTKV_ERR_UNSUPPORTED, "too many key tiles for one launch");
   const int grid = most < num_sms() ? (int)most : num_sms();
@@ -1326,7 +1328,7 @@ int32_t launch_tc(TreeTcArgs p, int max_kv, cudaStream_t st) {
 }
 
 template <int HD, bool F16>
-int32_t launch_tc_for(const TreeArgs &a, bool fp8, int max_kv, cudaStream_t st) {
+int32_t launch_tc_for(const TreeArgs &a, bool fp8, cudaStream_t st) {
   TreeTcArgs p{};
   p.a = a;
   const int rep = a.n_q / a.n_kv;
@@ -1338,9 +1340,9 @@ int32_t launch_tc_for(const TreeArgs &a, bool fp8, int max_kv, cudaStream_t st) 
   p.slot_rows = p.copies > 1 ? 128 : tc_slot_rows(a.total_new, a.n_q, a.n_kv);
   p.scale_log2 = a.scale * 1.4426950408889634f;
   p.store32 = ((uintptr_t)a.out & 31) == 0;
-  if (fp8) return launch_tc<HD, 1, F16, true>(p, max_kv, st);
+  if (fp8) return launch_tc<HD, 1, F16, true>(p, st);
   // more rows than one query tile holds: two tiles share the key tiles of a pass
-  return a.max_new > p.npt ? launch_tc<HD, 2, F16, false>(p, max_kv, st) : launch_tc<HD, 1, F16, false>(p, max_kv, st);
+  return a.max_new > p.npt ? launch_tc<HD, 2, F16, false>(p, st) : launch_tc<HD, 1, F16, false>(p, st);
 }
 
 }  // namespace
@@ -1381,25 +1383,27 @@ extern "C" int32_t swiftkv_tree_attention(const void *q, int64_t q_stride, int32
   if (need && (!scratch || scratch_bytes < need)) return report_error(SWIFTKV_ERR_WORKSPACE_SMALL, "scratch too small (see swiftkv_tree_attention_scratch_bytes)");
   unsigned int *status = op_status_word();
   if (!status) return report_error(SWIFTKV_ERR_CUDA, "no status word");
-  // (max_new: no sequence has more new tokens than there are, so a limit far above them neither picks the kernel's form nor sizes its grid)
+  // max_kv: lengths rounded up to whole tiles stay inside 32 bits.  max_new: no sequence has more new tokens than there are, so that a limit
+  // far above them neither picks the kernel's form nor sizes its grid.
   TreeArgs a{};
   a.q = q; a.q_stride = q_stride; a.k = k_cache; a.v = v_cache; a.k_scale = k_scale; a.v_scale = v_scale;
   a.blk = block_table; a.max_blocks = max_blocks; a.row0 = row0; a.past = n_past; a.cu = cu_new; a.mask = tree_mask; a.mask_words = mask_words;
   a.out = out; a.lse = lse; a.scratch = reinterpret_cast<float *>(scratch);
-  a.cache_rows = cache_rows; a.n_seqs = n_seqs; a.total_new = total_new; a.max_new = max_new < total_new ? max_new : total_new; a.max_kv = max_kv; a.n_q = n_q_heads; a.n_kv = n_kv_heads; a.hd = head_dim;
+  a.max_new = max_new < total_new ? max_new : total_new; a.max_kv = max_kv < TREE_MAX_KV ? max_kv : TREE_MAX_KV;
+  a.cache_rows = cache_rows; a.n_seqs = n_seqs; a.total_new = total_new; a.n_q = n_q_heads; a.n_kv = n_kv_heads; a.hd = head_dim;
   a.scale = softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)head_dim);
   a.status = status;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
   if (tc_supported(a, q_dtype != SWIFTKV_DTYPE_F32, fp8)) {
-    if (q_dtype == SWIFTKV_DTYPE_BF16) return head_dim == 64 ? launch_tc_for<64, false>(a, fp8, max_kv, st) : launch_tc_for<128, false>(a, fp8, max_kv, st);
-    return head_dim == 64 ? launch_tc_for<64, true>(a, fp8, max_kv, st) : launch_tc_for<128, true>(a, fp8, max_kv, st);
+    if (q_dtype == SWIFTKV_DTYPE_BF16) return head_dim == 64 ? launch_tc_for<64, false>(a, fp8, st) : launch_tc_for<128, false>(a, fp8, st);
+    return head_dim == 64 ? launch_tc_for<64, true>(a, fp8, st) : launch_tc_for<128, true>(a, fp8, st);
   }
   if (fp8) {
-    if (q_dtype == SWIFTKV_DTYPE_F32) return launch_simt<float, fp8e4>(a, max_kv, st);
-    if (q_dtype == SWIFTKV_DTYPE_BF16) return launch_simt<bf16, fp8e4>(a, max_kv, st);
-    return launch_simt<__half, fp8e4>(a, max_kv, st);
+    if (q_dtype == SWIFTKV_DTYPE_F32) return launch_simt<float, fp8e4>(a, st);
+    if (q_dtype == SWIFTKV_DTYPE_BF16) return launch_simt<bf16, fp8e4>(a, st);
+    return launch_simt<__half, fp8e4>(a, st);
   }
-  if (q_dtype == SWIFTKV_DTYPE_F32) return launch_simt<float, float>(a, max_kv, st);
-  if (q_dtype == SWIFTKV_DTYPE_BF16) return launch_simt<bf16, bf16>(a, max_kv, st);
-  return launch_simt<__half, __half>(a, max_kv, st);
+  if (q_dtype == SWIFTKV_DTYPE_F32) return launch_simt<float, float>(a, st);
+  if (q_dtype == SWIFTKV_DTYPE_BF16) return launch_simt<bf16, bf16>(a, st);
+  return launch_simt<__half, __half>(a, st);
 }

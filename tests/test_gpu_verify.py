@@ -452,6 +452,29 @@ def test_tree_attention_limits_of_a_large_server():
     P.op_status()
 
 
+@pytest.mark.parametrize("kind", ["bf16", "fp8", "f32"])
+def test_tree_attention_any_max_kv(kind):
+    import paper_2410_03960_b200 as P
+    c = tree_case(77, [(300, 3), (1500, 2)], 16, 4, 128, FF if kind == "f32" else BF, fp8=kind == "fp8")
+    out, lse = run_tree(dict(c, max_kv=(1 << 31) - 1))
+    check_tree(c, out, lse)
+    P.op_status()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp8"])
+def test_tree_attention_a_length_that_no_cache_has(kind):
+    """A committed length next to 2^31 is cut so that the keys are 2^30, and reported; what lies behind the table reads as zeros, which all
+    have score 0: the few hundred rows that are there carry 2^-21 of the probability."""
+    import paper_2410_03960_b200 as P
+    c = tree_case(78, [(300, 2)], 4, 1, 128, BF, fp8=kind == "fp8")
+    c["q"] = c["q"] * 0.01
+    out, lse = run_tree(dict(c, past=[(1 << 31) - 200], max_kv=(1 << 31) - 1))
+    assert (lse - 30 * math.log(2.0)).abs().max() <= 1e-4 and out.float().abs().max() <= 1e-4
+    with pytest.raises(P.SwiftKVError) as e:
+        P.op_status()
+    assert e.value.code == -6
+
+
 @pytest.mark.parametrize("kind", ["bf16", "f16", "fp8", "f32"])
 @pytest.mark.parametrize("heads", [(4, 1, 128), (6, 2, 64)], ids=str)
 def test_tree_attention_prompt_chunks(kind, heads):
