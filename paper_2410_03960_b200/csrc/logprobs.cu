@@ -723,8 +723,9 @@ using namespace skv;
 
 static int32_t check_logits(const void *logits, int64_t row_stride, int32_t rows, int32_t vocab, int32_t dtype, float temperature) {
   if (!logits) return report_error(SWIFTKV_ERR_INVALID_ARG, "null argument");
-  if (rows < 1 || rows > (1 << 26) || vocab < 1 || row_stride < vocab)
-    return report_error(SWIFTKV_ERR_INVALID_ARG, "bad shape (rows in [1, 2^26], vocab >= 1, row_stride >= vocab)");
+  // (the kernels count a row's elements in 32 bits, in steps of a block's work)
+  if (rows < 1 || rows > (1 << 26) || vocab < 1 || vocab > (1 << 30) || row_stride < vocab)
+    return report_error(SWIFTKV_ERR_INVALID_ARG, "bad shape (rows in [1, 2^26], vocab in [1, 2^30], row_stride >= vocab)");
   if (!(temperature > 0.f) || !(temperature < INFINITY)) return report_error(SWIFTKV_ERR_INVALID_ARG, "temperature must be positive and finite");
   if (dtype != SWIFTKV_DTYPE_F32 && dtype != SWIFTKV_DTYPE_BF16 && dtype != SWIFTKV_DTYPE_F16)
     return report_error(SWIFTKV_ERR_INVALID_ARG, "unknown dtype");

@@ -126,6 +126,13 @@ def test_token_logprobs_bwd(lib, bad):
     assert lib.swiftkv_token_logprobs_bwd(*{**LPB, **bad}.values()) == INVALID
 
 
+@pytest.mark.parametrize("bad", [dict(vocab=(1 << 30) + 1, stride=1 << 31), dict(vocab=(1 << 31) - 1, stride=1 << 31), dict(rows=(1 << 26) + 1)])
+def test_token_logprobs_of_more_than_32_bits_count(lib, bad):
+    """Rows whose last elements a block's step would carry past 2^31."""
+    assert lib.swiftkv_token_logprobs(*{**LP, **bad}.values()) == INVALID
+    assert lib.swiftkv_token_logprobs_bwd(*{**LPB, **bad, "out_stride": 1 << 31}.values()) == INVALID
+
+
 def test_wrappers_refuse_host_tensors(lib):
     import paper_2410_03960_b200 as P
     x, i = torch.zeros(2, 4), torch.zeros(2, dtype=torch.int32)
