@@ -528,6 +528,7 @@ int32_t swiftkv_rope_table(float *cos_tab, float *sin_tab, int32_t max_pos, int3
  *               e4m3 codes in the format of SWIFTKV_KV_FP8, quantized from the fp32 row (rows of at most 8192 values)
  *   slot_map  : int32 [n_tokens], cache row of every token (null: token t goes to row t); a row below 0 is not stored, one at or
  *               beyond cache_rows neither, and is reported.  No two tokens may name the same row
+ * An output may lie on its own input as stated (k_cache on k, v_cache on v too, without a slot map and where the rows coincide); any other overlap is refused.
  * Everything between load and store is fp32; stores to F16 round like a cast (no clamping).
  * Errors: INVALID_ARG, UNSUPPORTED (FP8 rows of more than 8192 values), CUDA. */
 int32_t swiftkv_qk_norm_rope(const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
@@ -538,7 +539,7 @@ int32_t swiftkv_qk_norm_rope(const void *q, int64_t q_stride, const void *k, int
 
 /* Its gradient: dq [n_tokens][n_q_heads][head_dim], dk [n_tokens][n_kv_heads][head_dim] (contiguous, `dtype`) are the gradients
  * of the rotated outputs; q, k, gains, positions and tables as given to the forward call.  dq_in, dk_in (contiguous, `dtype`;
- * may be dq / dk) receive the gradients of q and k; dq_gain, dk_gain (fp32 [head_dim]; null exactly where the gain is null)
+ * may be dq / dk, or q / k where those are contiguous; any other overlap is refused) receive the gradients of q and k; dq_gain, dk_gain (fp32 [head_dim]; null exactly where the gain is null)
  * those of the gains, summed over all tokens and heads in a fixed order (no atomics: results repeat bit for bit on one GPU
  * model).  scratch: >= swiftkv_qk_norm_rope_bwd_scratch_bytes(head_dim) bytes, 16-byte aligned, not shared with a call that may
  * run at the same time.  (v's gradient is the gradient of the stored values: nothing is computed.)
@@ -565,7 +566,8 @@ int32_t swiftkv_qk_norm_rope_bwd(const void *dq, const void *dk, const void *q, 
  *   max_new, max_kv : at least the largest number of new tokens and of n_past + new tokens of any sequence; a longer sequence is
  *                 cut there (n_past + new tokens at 2^30 in any case) and reported
  *   out         : [total_new][n_q_heads][head_dim] in q_dtype; lse (nullable): fp32 [total_new][n_q_heads], natural logarithm of the
- *                 softmax's denominator.  Rows of tokens that belong to no sequence are left as they were
+ *                 softmax's denominator.  Rows of tokens that belong to no sequence are left as they were.  out, lse and scratch must not overlap
+ *                 q, the cache or one another
  *   softmax_scale : 0 means 1/sqrt(head_dim)
  *   scratch     : >= swiftkv_tree_attention_scratch_bytes(...) bytes (may be null where that is 0), 256-byte aligned, not shared with
  *                 a call that may run at the same time; sufficient for any smaller total_new and max_kv too

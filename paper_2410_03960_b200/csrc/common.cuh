@@ -128,6 +128,25 @@ int ensure_dynamic_smem(const void *kernel, int bytes);
 // the current device's status word of the stand-alone operators (null on a CUDA error)
 unsigned int *op_status_word();
 
+// rows of a caller's tensor, for the checks of arguments: n rows of `width` bytes, `stride` bytes apart
+struct ByteRows { const void *p; size_t n, stride, width; };
+// whether two share a byte (of differently strided ones that lie within each other: yes)
+inline bool overlap(ByteRows a, ByteRows b) {
+  auto whole = [](const ByteRows &x) { return x.n == 1 || x.stride == x.width; };
+  if (whole(a) && !whole(b)) { const ByteRows t = a; a = b; b = t; }
+  const uintptr_t a0 = reinterpret_cast<uintptr_t>(a.p), b0 = reinterpret_cast<uintptr_t>(b.p);
+  const uintptr_t a1 = a0 + (a.n - 1) * a.stride + a.width, b1 = b0 + (b.n - 1) * b.stride + b.width;
+  if (a0 >= b1 || b0 >= a1) return false;
+  if (whole(a)) return true;
+  if (whole(b)) {                                  // the first row of a that ends behind b's start
+    const size_t i = b0 >= a0 + a.width ? (b0 - a0 - a.width) / a.stride + 1 : 0;
+    return i < a.n && a0 + i * a.stride < b1;
+  }
+  if (a.stride != b.stride) return true;
+  const size_t ahead = b0 >= a0 ? (b0 - a0) % a.stride : (a.stride - (a0 - b0) % a.stride) % a.stride;      // of b's rows before a's
+  return ahead < a.width || ahead + b.width > a.stride;
+}
+
 // sets the calling thread's swiftkv_last_error() text and returns `code` (defined with the C ABI)
 int32_t report_error(int32_t code, const char *msg);
 

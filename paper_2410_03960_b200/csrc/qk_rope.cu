@@ -692,6 +692,16 @@ extern "C" int32_t swiftkv_qk_norm_rope(const void *q, int64_t q_stride, const v
   if (!(eps >= 0.f)) return report_error(SWIFTKV_ERR_INVALID_ARG, "eps must not be negative");
   if (misaligned(q, dtype) || misaligned(k, dtype) || misaligned(v, dtype) || misaligned(q_out, dtype) || (!k_scale && (misaligned(k_cache, dtype) || misaligned(v_cache, dtype))))
     return report_error(SWIFTKV_ERR_INVALID_ARG, "misaligned pointer");
+  // in place a head is read by the threads that write it; any other overlap is not
+  const size_t es = dtype == SWIFTKV_DTYPE_F32 ? 4 : 2, T = (size_t)n_tokens;
+  const ByteRows rq{q, T, q_stride * es, nq * es}, rk{k, T, k_stride * es, nkv * es}, rv{v, T, v_stride * es, nkv * es}, ro{q_out, T, q_out_stride * es, nq * es};
+  const size_t plane = (size_t)cache_rows * nkv * (k_scale ? 1 : es);
+  const ByteRows ck{k_cache, 1, plane, plane}, cv{v_cache, 1, plane, plane};
+  auto rows_in_place = [&](const void *cache, const void *x, int64_t stride) { return cache == x && !slot_map && !k_scale && (stride == nkv || n_tokens == 1); };
+  if ((overlap(ro, rq) && !(q_out == q && (q_out_stride == q_stride || n_tokens == 1))) || overlap(ro, rk) || overlap(ro, rv) || overlap(ro, ck) || overlap(ro, cv) ||
+      overlap(ck, cv) || overlap(ck, rq) || overlap(cv, rq) || overlap(ck, rv) || overlap(cv, rk) || (overlap(ck, rk) && !rows_in_place(k_cache, k, k_stride)) ||
+      (overlap(cv, rv) && !rows_in_place(v_cache, v, v_stride)))
+    return report_error(SWIFTKV_ERR_INVALID_ARG, "an output overlaps an input other than in place, or another output");
   unsigned int *status = op_status_word();
   if (!status) return report_error(SWIFTKV_ERR_CUDA, "no status word");
   RopeArgs a{q, k, v, q_stride, k_stride, v_stride, q_gain, k_gain, positions, cos_tab, sin_tab, slot_map, q_out, k_cache, v_cache, q_out_stride,
@@ -724,6 +734,14 @@ extern "C" int32_t swiftkv_qk_norm_rope_bwd(const void *dq, const void *dk, cons
       (reinterpret_cast<uintptr_t>(scratch) & 15))
     return report_error(SWIFTKV_ERR_INVALID_ARG, "misaligned pointer");
   if (scratch_bytes < swiftkv_qk_norm_rope_bwd_scratch_bytes(head_dim)) return report_error(SWIFTKV_ERR_WORKSPACE_SMALL, "scratch too small");
+  // in place a head is read by the threads that write it; any other overlap is not
+  const size_t es = dtype == SWIFTKV_DTYPE_F32 ? 4 : 2, T = (size_t)n_tokens;
+  const int64_t nq = (int64_t)n_q_heads * head_dim, nkv = (int64_t)n_kv_heads * head_dim;
+  const ByteRows rq{q, T, q_stride * es, nq * es}, rk{k, T, k_stride * es, nkv * es}, dyq{dq, T, nq * es, nq * es}, dyk{dk, T, nkv * es, nkv * es},
+      oq{dq_in, T, nq * es, nq * es}, ok{dk_in, T, nkv * es, nkv * es};
+  if ((overlap(oq, dyq) && dq_in != dq) || (overlap(oq, rq) && !(dq_in == q && (q_stride == nq || n_tokens == 1))) || overlap(oq, dyk) || overlap(oq, rk) ||
+      (overlap(ok, dyk) && dk_in != dk) || (overlap(ok, rk) && !(dk_in == k && (k_stride == nkv || n_tokens == 1))) || overlap(ok, dyq) || overlap(ok, rq) || overlap(oq, ok))
+    return report_error(SWIFTKV_ERR_INVALID_ARG, "an output overlaps an input other than in place, or another output");
   unsigned int *status = op_status_word();
   if (!status) return report_error(SWIFTKV_ERR_CUDA, "no status word");
   RopeBwdArgs a{dq, dk, q, k, q_stride, k_stride, q_gain, k_gain, positions, cos_tab, sin_tab, dq_in, dk_in, reinterpret_cast<float *>(scratch),

@@ -1381,6 +1381,17 @@ extern "C" int32_t swiftkv_tree_attention(const void *q, int64_t q_stride, int32
     return report_error(SWIFTKV_ERR_INVALID_ARG, "misaligned pointer");
   const size_t need = swiftkv_tree_attention_scratch_bytes(total_new, max_kv, n_q_heads, head_dim);
   if (need && (!scratch || scratch_bytes < need)) return report_error(SWIFTKV_ERR_WORKSPACE_SMALL, "scratch too small (see swiftkv_tree_attention_scratch_bytes)");
+  // a query tile is read by every block that has keys for it, also after another has written its rows
+  const size_t row = (size_t)n_q_heads * head_dim * es, plane = (size_t)cache_rows * n_kv_heads * head_dim * kes;
+  auto part = [](const void *p, size_t bytes) { return ByteRows{p, 1, bytes, bytes}; };
+  const ByteRows in[] = {{q, (size_t)total_new, (size_t)q_stride * es, row}, part(k_cache, plane), part(v_cache, plane)};
+  const ByteRows outs[] = {part(out, total_new * row), part(lse, lse ? (size_t)total_new * n_q_heads * sizeof(float) : 0), part(scratch, need)};
+  for (int i = 0; i < 3; ++i) {
+    if (!outs[i].width) continue;
+    for (int j = 0; j < 3; ++j)
+      if (overlap(outs[i], in[j]) || (j < i && outs[j].width && overlap(outs[i], outs[j])))
+        return report_error(SWIFTKV_ERR_INVALID_ARG, "out, lse or scratch overlaps q, the cache or another of them");
+  }
   unsigned int *status = op_status_word();
   if (!status) return report_error(SWIFTKV_ERR_CUDA, "no status word");
   // max_kv: lengths rounded up to whole tiles stay inside 32 bits.  max_new: no sequence has more new tokens than there are, so that a limit

@@ -209,6 +209,44 @@ def test_qk_norm_rope_in_place_and_unaligned():
     P.op_status()
 
 
+@pytest.mark.parametrize("dt", [BF, HF, FF])
+@pytest.mark.parametrize("T,n_q,n_kv,hd", [(1, 4, 2, 128), (700, 8, 2, 64), (2100, 4, 4, 128), (90, 3, 2, 80)])
+def test_qk_norm_rope_on_its_inputs(T, n_q, n_kv, hd, dt):
+    """Queries, keys and values where they are: without a slot map every row is its own place; and the gradients over q and k."""
+    import paper_2410_03960_b200 as P
+    g, q, k, v, pos, (qg, kg) = rope_inputs(T, n_q, n_kv, hd, dt, T, strided=False)
+    q, k, v = q.contiguous(), k.contiguous(), v.contiguous()
+    cos, sin = P.rope_table(131072, hd, THETA)
+    dq, dk = (torch.randn((T, n, hd), generator=g, device="cuda").to(dt) for n in (n_q, n_kv))
+    kc, vc = torch.empty_like(k), torch.empty_like(v)
+    qo = P.qk_norm_rope(q, k, v, pos, cos, sin, q_gain=qg, k_gain=kg, eps=EPS, k_cache=kc, v_cache=vc)
+    q2, k2, v2 = q.clone(), k.clone(), v.clone()
+    P.qk_norm_rope(q2, k2, v2, pos, cos, sin, q_gain=qg, k_gain=kg, eps=EPS, k_cache=k2, v_cache=v2, q_out=q2)
+    assert torch.equal(q2, qo) and torch.equal(k2, kc) and torch.equal(v2, v) and torch.equal(vc, v)
+    want = P.qk_norm_rope_bwd(dq, dk, q, k, pos, cos, sin, q_gain=qg, k_gain=kg, eps=EPS)
+    q2, k2 = q.clone(), k.clone()
+    got = P.qk_norm_rope_bwd(dq, dk, q2, k2, pos, cos, sin, q_gain=qg, k_gain=kg, eps=EPS, out=(q2, k2))
+    P.op_status()
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+
+
+def test_overlaps_are_refused():
+    import paper_2410_03960_b200 as P
+    _, q, k, v, pos, _ = rope_inputs(9, 4, 2, 64, BF, 3)
+    cos, sin = P.rope_table(131072, 64, THETA)
+    flat = torch.empty(9 * 4 * 64 + 64, dtype=BF, device="cuda")
+    a, b = flat[:-64].view(9, 4, 64), flat[64:].view(9, 4, 64)
+    kc = torch.empty_like(k, memory_format=torch.contiguous_format)
+    with pytest.raises(P.SwiftKVError):
+        P.qk_norm_rope(a, k, v, pos, cos, sin, k_cache=kc, v_cache=torch.empty_like(kc), q_out=b)
+    with pytest.raises(P.SwiftKVError):
+        P.qk_norm_rope(q, k, v, pos, cos, sin, k_cache=kc, v_cache=kc)
+    c = tree_case(5, [(90, 9)], 4, 2, 64, BF)
+    with pytest.raises(P.SwiftKVError):
+        run_tree(c, out=c["q"])
+
+
 def test_qk_norm_rope_reports_bad_indices():
     import paper_2410_03960_b200 as P
     _, q, k, v, pos, _ = rope_inputs(4, 4, 2, 64, BF, 6, max_pos=50)
