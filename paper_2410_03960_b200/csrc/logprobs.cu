@@ -605,6 +605,9 @@ __global__ void __launch_bounds__(LP_THREADS + 32, 2) token_logprobs_kernel(LpAr
       cluster.sync();
     }
   }
+  // giving up: copies under way land before the ring is given back (these waits are bounded too)
+  if (tid == 0 && !alive)
+    for (int i = max(0, p_count - LP_STAGES); i < p_count; ++i) tc::mbar_wait(tc::smem_u32(&sh.full[i % LP_STAGES]), (i / LP_STAGES) & 1);
 }
 
 // d logits = ( g_lp (1[v = t] - p_v) - g_H p_v (log p_v + H) ) / T  with p = exp(z - lse): elementwise, one read and one

@@ -443,6 +443,8 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
   volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
   volatile int *bad_item = reinterpret_cast<volatile int *>(tmem_slot + 2);      // [2]
   int *start = reinterpret_cast<int *>(tmem_slot + 4);                           // first sequence, units before the range in it
+  int *issued = start + 2;                                                       // giving up: K, V (FP8: codes), query tiles that were requested
+  uint64_t *drained = reinterpret_cast<uint64_t *>(tmem_slot + 10);
   float2 *ml = reinterpret_cast<float2 *>(smem + L::ML);                         // [item & 1][stream][128]
   float *scales = reinterpret_cast<float *>(smem + L::SC);                       // [tile & 3][K, V, log2 V][128], then [item & 1][128]
 
@@ -498,6 +500,7 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
       tc::mbar_init(tc::smem_u32(&s_half[s]), 1);
     }
     tc::mbar_init(tc::smem_u32(q_ready), 4);
+    tc::mbar_init(tc::smem_u32(drained), 1);
     tc::mbar_init(tc::smem_u32(&q_scaled[0]), 4);
     tc::mbar_init(tc::smem_u32(&q_scaled[1]), 4);
     for (int s = 0; s < 4; ++s) {
@@ -573,6 +576,8 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
           if (!ok || !it.next(a)) break;
           entry = tile_entry(a, it.b, it.kt0);
         } while (true);
+        issued[0] = FP8 ? cc : kc;
+        issued[1] = vc;
       }
     } else if (warp == 1) {
       // -------------------------------------------------------------------- MMA issuer (one elected lane), query tiles
@@ -660,6 +665,7 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
         more = ok && it.next(a);
         if (more && leader) load_q();
       } while (more);
+      issued[2] = item;
     } else if (FP8 && warp == 2) {
       // -------------------------------------------------------------------- row scales, four keys per lane, a tile ahead of their use
       int tile = 0;
@@ -1138,6 +1144,27 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
   }
   tc::tc_fence_before_sync();
   __syncthreads();
+  if (*abort_flag) {
+    // a wait ran out: copies and products under way end before shared and tensor memory are given back (these waits are bounded too)
+    if (warp == 0 && lane == 0) {
+      auto landed = [&](uint64_t *full, int places, int n) {
+        for (int i = max(0, n - places); i < n; ++i) tc::mbar_wait(tc::smem_u32(&full[i % places]), (i / places) & 1);
+      };
+      if constexpr (FP8) {
+        landed(c_full, L::CS, issued[0]);
+      } else {
+        landed(k_full, L::KS, issued[0]);
+        landed(v_full, L::VS, issued[1]);
+      }
+      landed(q_full, 1, issued[2]);
+    }
+    if (warp == 1) {
+      if (tc::elect_one()) tc::umma_commit(tc::smem_u32(drained));
+      __syncwarp();
+      tc::mbar_wait(tc::smem_u32(drained), 0);
+    }
+    __syncthreads();
+  }
   if (warp == 1) {
     __syncwarp();
     tc::tc_fence_after_sync();
