@@ -55,10 +55,14 @@ class _On:
 
 
 def op_status(device=None, stream: Optional[torch.cuda.Stream] = None) -> None:
-    """swiftkv_op_status: synchronises the stream; raises SwiftKVError for what the stand-alone operators met on the device since the last call."""
-    if stream is not None and device is None:
-        device = stream.device
-    index = torch.cuda.current_device() if device is None else torch.device(device).index or 0
+    """swiftkv_op_status: synchronises the stream; raises SwiftKVError for what the stand-alone operators met on the device (default: the
+    stream's, else the current one) since the last call."""
+    index = None if device is None else torch.device(device).index
+    if stream is not None:
+        if index is not None and index != stream.device_index:
+            raise ValueError("the stream belongs to another device")
+        index = stream.device_index
+    index = torch.cuda.current_device() if index is None else index
     with torch.cuda.device(index):
         _check(load_library().swiftkv_op_status((stream or torch.cuda.current_stream()).cuda_stream))
 
