@@ -1,12 +1,14 @@
-"""Builds the CUDA library in-tree:  python -m paper_2410_03960_b200.build
+"""Builds the CUDA library in-tree:  python -m paper_2410_03960_b200.build [--force] [--library]
 
-One nvcc invocation compiles every .cu under csrc/ for sm_100a into libswiftkv.so next to this file; g++ compiles
-csrc/verify_py.cpp, a Python extension against torch's headers, into _verify.so.  nvcc cross-compiles without a GPU, so this also
-runs on a CPU-only machine.
+One nvcc invocation compiles every .cu under csrc/ for sm_100a into libswiftkv.so next to this file; then g++ compiles
+csrc/verify_py.cpp, a Python extension against torch's headers, into _verify.so.  --library builds the C library alone, which needs
+neither torch nor Python's headers.  nvcc cross-compiles without a GPU, so this also runs on a CPU-only machine.
 """
 from __future__ import annotations
 
+import importlib.util
 import os
+import shutil
 import subprocess
 import sys
 
@@ -20,11 +22,22 @@ NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", 
               "-Xcompiler", "-fPIC", "-shared", "-Xptxas", "-v"]
 
 
+def _nvcc() -> str:
+    return os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
+
+
+def _torch_version_file() -> str:
+    spec = importlib.util.find_spec("torch")
+    return os.path.join(os.path.dirname(spec.origin), "version.py") if spec and spec.origin else ""
+
+
 def _ext_stale() -> bool:
+    """Older than its sources or than the torch that it would be loaded into (one of another version refuses to load, see verify.py)."""
     if not os.path.exists(EXT):
         return True
     t = os.path.getmtime(EXT)
-    return any(os.path.getmtime(d) > t for d in (os.path.join(CSRC, "verify_py.cpp"), os.path.join(HERE, "..", "include", "swiftkv.h")))
+    deps = (os.path.join(CSRC, "verify_py.cpp"), os.path.join(HERE, "..", "include", "swiftkv.h"), _torch_version_file())
+    return any(os.path.exists(d) and os.path.getmtime(d) > t for d in deps)
 
 
 def build_ext(verbose: bool = False) -> str:
@@ -33,10 +46,12 @@ def build_ext(verbose: bool = False) -> str:
 
     import torch
     torch_dir = os.path.dirname(torch.__file__)
-    inc = [os.path.join(torch_dir, "include"), os.path.join(torch_dir, "include", "torch", "csrc", "api", "include"), "/usr/local/cuda/include",
-           sysconfig.get_paths()["include"]]
+    nvcc = os.path.realpath(shutil.which(_nvcc()) or _nvcc())
+    inc = [os.path.join(torch_dir, "include"), os.path.join(torch_dir, "include", "torch", "csrc", "api", "include"),
+           os.path.join(os.path.dirname(os.path.dirname(nvcc)), "include"), sysconfig.get_paths()["include"]]
     libs = os.path.join(torch_dir, "lib")
-    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"] + [f"-I{i}" for i in inc] + \
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           f'-DSWIFTKV_TORCH="{torch.__version__}"'] + [f"-I{i}" for i in inc] + \
         [os.path.join(CSRC, "verify_py.cpp"), "-o", EXT, f"-L{libs}", "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
     proc = subprocess.run(cmd, capture_output=True, text=True)
     if verbose or proc.returncode != 0:
@@ -55,12 +70,18 @@ def _stale() -> bool:
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
+    """The library, then the extension: what fails of the second leaves the first built."""
+    build_library(force, verbose)
     if force or _ext_stale():
         build_ext(verbose)
+    return LIB
+
+
+def build_library(force: bool = False, verbose: bool = False) -> str:
+    """csrc/*.cu -> libswiftkv.so."""
     if not force and not _stale():
         return LIB
-    nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
-    cmd = [nvcc] + NVCC_FLAGS + [os.path.join(CSRC, s) for s in SOURCES] + ["-o", LIB]
+    cmd = [_nvcc()] + NVCC_FLAGS + [os.path.join(CSRC, s) for s in SOURCES] + ["-o", LIB]
     proc = subprocess.run(cmd, capture_output=True, text=True)
     if verbose or proc.returncode != 0:
         sys.stderr.write(proc.stdout + proc.stderr)
@@ -78,4 +99,4 @@ def build(force: bool = False, verbose: bool = False) -> str:
 
 
 if __name__ == "__main__":
-    print(build(force="--force" in sys.argv, verbose=True))
+    print((build_library if "--library" in sys.argv else build)(force="--force" in sys.argv, verbose=True))

@@ -370,4 +370,8 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_verify", "marshalling of the veri
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__verify(void) { return PyModule_Create(&module); }
+PyMODINIT_FUNC PyInit__verify(void) {
+  PyObject *m = PyModule_Create(&module);
+  if (m && PyModule_AddStringConstant(m, "built_for_torch", SWIFTKV_TORCH)) Py_CLEAR(m);
+  return m;
+}

@@ -31,7 +31,13 @@ def _load():
         path = os.path.join(os.path.dirname(os.path.abspath(__file__)), "_verify.so")
         if not os.path.exists(path):
             raise RuntimeError(f"{path} is missing: build it with `python -m paper_2410_03960_b200.build`")
-        from . import _verify
+        try:
+            from . import _verify
+            built_for = getattr(_verify, "built_for_torch", "another version")
+        except ImportError as e:
+            raise RuntimeError(f"{path} does not load into torch {torch.__version__} (rebuild it with `python -m paper_2410_03960_b200.build --force`): {e}") from e
+        if built_for != torch.__version__:
+            raise RuntimeError(f"{path} was built for torch {built_for}, this is {torch.__version__}: rebuild it with `python -m paper_2410_03960_b200.build --force`")
         _verify.bind(SwiftKVError, {name: C.cast(getattr(lib, name), C.c_void_p).value for name in _ADDRESSES})
         _EXT = _verify
     return _EXT
