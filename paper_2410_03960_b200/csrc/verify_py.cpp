@@ -229,6 +229,7 @@ PyObject *qk_norm_rope(PyObject *, PyObject *const *a, Py_ssize_t argc) {
     const Tensor out = a[14] == Py_None ? on.make(q.sizes(), r.type) : tensor(a[14], "q_out");
     const Heads ho = heads(on, out, "q_out", r.type);
     if (out.sizes() != q.sizes()) throw Refused("q_out must have q's shape");
+    if (r.n == 0) return THPVariable_Wrap(out);
     check(p_swiftkv_qk_norm_rope(r.q.p, r.q.stride, r.k.p, r.k.stride, hv.p, hv.stride, r.code, r.n, r.n_q, r.n_kv, r.hd, r.q_gain, r.k_gain, f32(a[8]),
                                  static_cast<int32_t *>(r.pos), static_cast<float *>(r.cos), static_cast<float *>(r.sin), r.max_pos, ho.p, ho.stride, c.k, c.v,
                                  c.k_scale, c.v_scale, c.rows, static_cast<int32_t *>(p_slots), on.stream()));
@@ -248,6 +249,11 @@ PyObject *qk_norm_rope_bwd(PyObject *, PyObject *const *a, Py_ssize_t argc) {
     Tensor gq, gk;
     if (r.q_gain) gq = on.make({r.hd}, at::kFloat);
     if (r.k_gain) gk = on.make({r.hd}, at::kFloat);
+    if (r.n == 0) {
+      if (r.q_gain) gq.zero_();
+      if (r.k_gain) gk.zero_();
+      return Py_BuildValue("NNNN", THPVariable_Wrap(oq), THPVariable_Wrap(ok), r.q_gain ? THPVariable_Wrap(gq) : none(), r.k_gain ? THPVariable_Wrap(gk) : none());
+    }
     const size_t bytes = p_swiftkv_qk_norm_rope_bwd_scratch_bytes(r.hd);
     const Tensor scratch = on.make({(int64_t)(bytes ? bytes : 1)}, at::kByte);
     check(p_swiftkv_qk_norm_rope_bwd(dq, dk, r.q.p, r.q.stride, r.k.p, r.k.stride, r.code, r.n, r.n_q, r.n_kv, r.hd, r.q_gain, r.k_gain, f32(a[9]),
@@ -287,6 +293,7 @@ PyObject *tree_attention(PyObject *, PyObject *const *a, Py_ssize_t argc) {
     const Tensor *lse = optional_tensor(a[14], "lse");
     float *p_lse = lse ? static_cast<float *>(whole(on, *lse, "lse", {t, n_q}, at::kFloat)) : nullptr;
     const int32_t max_new = i32(a[5], "max_new"), max_kv = i32(a[6], "max_kv");
+    if (t == 0) return THPVariable_Wrap(out);
     const size_t bytes = p_swiftkv_tree_attention_scratch_bytes(i32(t, "tokens"), max_kv, i32(n_q, "heads"), i32(hd, "head_dim"));
     Tensor scratch;
     if (bytes) scratch = on.make({(int64_t)bytes}, at::kByte);
@@ -318,8 +325,10 @@ PyObject *token_logprobs(PyObject *, PyObject *const *a, Py_ssize_t argc) {
       ids = static_cast<int32_t *>(whole(on, tensor(a[7], "top_ids"), "top_ids", {r.rows, k}, at::kInt));
       lps = static_cast<float *>(whole(on, tensor(a[8], "top_logprobs"), "top_logprobs", {r.rows, k}, at::kFloat));
     }
-    check(p_swiftkv_token_logprobs(r.p, r.stride, r.code, targets ? static_cast<int32_t *>(vec(on, *targets, "targets", r.rows)) : nullptr, r.rows, r.vocab, f32(a[3]),
-                                   k, f(4, "logprob"), f(5, "entropy"), f(6, "lse"), ids, lps, on.stream()));
+    int32_t *tgt = targets ? static_cast<int32_t *>(vec(on, *targets, "targets", r.rows)) : nullptr;
+    float *logprob = f(4, "logprob"), *entropy = f(5, "entropy"), *lse = f(6, "lse");
+    if (r.rows == 0) return none();
+    check(p_swiftkv_token_logprobs(r.p, r.stride, r.code, tgt, r.rows, r.vocab, f32(a[3]), k, logprob, entropy, lse, ids, lps, on.stream()));
     return none();
   });
 }
@@ -339,6 +348,7 @@ PyObject *token_logprobs_bwd(PyObject *, PyObject *const *a, Py_ssize_t argc) {
     const Tensor out = a[7] == Py_None ? on.make(x.sizes(), x.scalar_type()) : tensor(a[7], "out");
     const Rows o = rows_of(on, out, "out");
     if (o.code != r.code || o.rows != r.rows || o.vocab != r.vocab) throw Refused("out must have the logits' shape, type and device");
+    if (r.rows == 0) return THPVariable_Wrap(out);
     check(p_swiftkv_token_logprobs_bwd(r.p, r.stride, r.code, targets, r.rows, r.vocab, f32(a[6]), lse, entropy, g_lp, g_h, o.p, o.stride, on.stream()));
     return THPVariable_Wrap(out);
   });

@@ -4,7 +4,7 @@ gradient), tree_attention, token_logprobs (and its gradient).  include/swiftkv.h
 Argument checks and marshalling only, done in csrc/verify_py.cpp (these calls sit in a serving loop; from Python they would cost
 more than the smallest kernels).  Every call queues its work on `stream` (default: the current stream of the tensors' device) and
 returns without synchronising; outputs and scratch that the caller does not bring are allocated on that stream, so that torch does
-not hand their memory to another one too early.  ValueError: tensors that do not fit together; SwiftKVError: what the library
+not hand their memory to another one too early.  No tokens or no rows: nothing is queued, and results are empty (gain gradients zero).  ValueError: tensors that do not fit together; SwiftKVError: what the library
 refuses."""
 from __future__ import annotations
 

@@ -1136,3 +1136,31 @@ def test_the_gradients_captured_and_replayed():
         graph.replay()
         for a, b in zip(got, both()):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dt", [BF, FF])
+def test_no_tokens_and_no_rows(dt):
+    """A step in which nothing is drafted: empty results of the right shapes, caches as they were; bad arguments are refused all the same."""
+    import paper_2410_03960_b200 as P
+    e = lambda *shape: torch.empty(shape, dtype=dt, device="cuda")  # noqa: E731
+    q, k, cos, sin = e(0, 4, 64), e(0, 2, 64), *P.rope_table(16, 64, THETA)
+    kc, vc, gain = e(256, 2, 64).fill_(3), e(256, 2, 64).fill_(3), e(64).fill_(1)
+    plan = P.plan_pages(i32([100]), i32([0]), i32([1]), i32([[0]]), i32([1]), i32([1]), max_tokens=0)
+    assert plan["info"].tolist() == [0, 0, 0, 100]
+    out = P.qk_norm_rope(q, k, k, plan["positions"], cos, sin, q_gain=gain, k_gain=gain, k_cache=kc, v_cache=vc, slot_map=plan["slot_map"])
+    assert out.shape == (0, 4, 64) and out.dtype == dt and (kc == 3).all() and (vc == 3).all()
+    dq, dk, gq, gk = P.qk_norm_rope_bwd(q, k, q, k, plan["positions"], cos, sin, q_gain=gain)
+    assert dq.shape == (0, 4, 64) and dk.shape == (0, 2, 64) and (gq == 0).all() and gq.shape == (64,) and gk is None
+    lse = torch.empty((0, 4), device="cuda")
+    assert P.tree_attention(q, kc, vc, i32([100]), plan["cu_new"], 8, 1000, block_table=plan["block_table"], lse=lse).shape == (0, 4, 64)
+    x, none = e(0, 300), torch.empty(0, device="cuda")
+    got = P.token_logprobs(x, i32([]), top_k=3)
+    assert got["lse"].shape == (0,) and got["top_ids"].shape == (0, 3)
+    assert P.token_logprobs_bwd(x, i32([]), none, None, none).shape == (0, 300)
+    with pytest.raises(ValueError):
+        P.qk_norm_rope(q, k, k, i32([1]), cos, sin, k_cache=kc, v_cache=vc)
+    with pytest.raises(ValueError):
+        P.tree_attention(q, kc, vc, i32([100]), i32([0]), 8, 1000, block_table=plan["block_table"])
+    with pytest.raises(ValueError):
+        P.token_logprobs(x, i32([1]))
+    P.op_status()
