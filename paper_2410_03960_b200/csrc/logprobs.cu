@@ -41,6 +41,9 @@ constexpr int LP_STAGES = 3;
 constexpr int LP_SMEM = LP_STAGES * LP_CHUNK * 16;
 constexpr float LP_RESCALE = 16.f;           // the reference moves when the sums could grow by more than 2^16
 constexpr float LOWEST = -3.0e38f;
+// Largest |x c| whose exponents are formed as x c - r: the product's rounding, which r has and the fused multiply-add has not, is up to
+// half a step, 64 here, and sums of 2^64 are still far from infinite.
+constexpr float LP_FAR = 1073741824.f;
 
 __device__ __forceinline__ float exp2_approx(float x) {
   float y;
@@ -487,9 +490,15 @@ __global__ void __launch_bounds__(LP_THREADS + 32, 2) token_logprobs_kernel(LpAr
       const uint32_t n = atomicAdd(&sh.n_notes[par], 1u);
       if (n < LP_NOTES) sh.note[par][n] = make_uint2((uint32_t)i, order_key(v));
     };
-    auto refer = [&](float vmax) {
+    // Makes room for logits up to vmax; false: they are not to be added.  Those far below zero (masked ones) have no probability beside any
+    // other, and a thread whose largest is far from zero forms its sums anew in the end.
+    auto refer = [&](float vmax) -> bool {
       m = fmaxf(m, vmax);
       const float y = vmax * c;
+      if (!(fabsf(y) <= LP_FAR)) {
+        if (vmax != vmax) l2.f[0] = vmax;
+        return false;
+      }
       if (y - r > LP_RESCALE) {
         if (r != -INFINITY) {
           lp_move(l2.f[0], s2.f[0], r - y);
@@ -497,6 +506,7 @@ __global__ void __launch_bounds__(LP_THREADS + 32, 2) token_logprobs_kernel(LpAr
         }
         r = y;
       }
+      return true;
     };
     auto add = [&](float d) {
       d = max_nan(d, LOWEST);                               // (-inf would make the product below NaN)
@@ -520,21 +530,21 @@ __global__ void __launch_bounds__(LP_THREADS + 32, 2) token_logprobs_kernel(LpAr
           if (v0 + u * LP_THREADS + tid >= rw.v_end) raw[u] = make_uint4(none, none, none, none);
       }
       const float vmax = chunk_max(raw, (const T *)nullptr);
-      refer(vmax);
-      const float ref = r == -INFINITY ? 0.f : r;
+      if (refer(vmax)) {
 #pragma unroll
-      for (int u = 0; u < LP_UNROLL; ++u) {
-        float e[N];
-        clamp_vec(raw[u], a.low, (const T *)nullptr);
-        LpVec<T>::unpack(raw[u], e);
+        for (int u = 0; u < LP_UNROLL; ++u) {
+          float e[N];
+          clamp_vec(raw[u], a.low, (const T *)nullptr);
+          LpVec<T>::unpack(raw[u], e);
 #pragma unroll
-        for (int i = 0; i < N; i += 2) {
-          F2 d = fma2(F2{{e[i], e[i + 1]}}, F2{{c, c}}, F2{{-ref, -ref}}), p;
-          if (sizeof(T) == 4) { d.f[0] = max_nan(d.f[0], LOWEST); d.f[1] = max_nan(d.f[1], LOWEST); }
-          p.f[0] = exp2_approx(d.f[0]);
-          p.f[1] = exp2_approx(d.f[1]);
-          l2 = add2(l2, p);
-          s2 = fma2(p, d, s2);
+          for (int i = 0; i < N; i += 2) {
+            F2 d = fma2(F2{{e[i], e[i + 1]}}, F2{{c, c}}, F2{{-r, -r}}), p;
+            if (sizeof(T) == 4) { d.f[0] = max_nan(d.f[0], LOWEST); d.f[1] = max_nan(d.f[1], LOWEST); }
+            p.f[0] = exp2_approx(d.f[0]);
+            p.f[1] = exp2_approx(d.f[1]);
+            l2 = add2(l2, p);
+            s2 = fma2(p, d, s2);
+          }
         }
       }
       if (TOP) {
@@ -567,15 +577,14 @@ __global__ void __launch_bounds__(LP_THREADS + 32, 2) token_logprobs_kernel(LpAr
       __syncwarp();
       if (lane == 0) tc::mbar_arrive(tc::smem_u32(&sh.empty[st]));
     }
-    if (edge >= 0) { refer(edge_v); add(fmaf(edge_v, c, r == -INFINITY ? 0.f : -r)); }
+    if (edge >= 0 && refer(edge_v)) add(fmaf(edge_v, c, -r));
     float l = l2.f[0] + l2.f[1], s = s2.f[0] + s2.f[1];
     if (m != -INFINITY) {
-      if (fabsf(m * c) < 1e37f && m * c > a.low * c + 1024.f) {
+      if (fabsf(m * c) <= LP_FAR && m * c > a.low * c + 1024.f) {
         lp_move(l, s, r - m * c);
         lp_move(l, s, fmaf(-m, c, m * c));                  // (m c is a rounded product: what it lacks)
       } else {
-        // logits near the type's limits, whose products with c are not finite or which a lifted -inf would reach: this thread's once
-        // more, differences first
+        // logits whose products with c are too large, or which a lifted -inf would reach: this thread's once more, differences first
         l2.f[0] = s2.f[0] = 0.f;
         for (int at = rw.v_begin + tid; at < rw.v_end; at += LP_THREADS) {
           float e[N];

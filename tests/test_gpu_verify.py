@@ -910,6 +910,57 @@ def test_token_logprobs_a_nan_in_every_vector(dt, vocab):
     assert got["top_ids"].tolist() == np.argsort(-np.nan_to_num(f64(x), nan=1e30), 1, kind="stable")[:, :k].tolist()
 
 
+@pytest.mark.parametrize("dt", [FF, BF, HF])
+@pytest.mark.parametrize("vocab", [18, 3001, 40000])
+@pytest.mark.parametrize("temperature", [0.7, 1.0, 1.5, 3.0, 50.0])
+def test_token_logprobs_masked_by_low_values(dt, vocab, temperature):
+    """Logits masked by the type's lowest value, or by others near it: ahead of the rest, behind them, in between, all but one, all.  (As
+    a probability every one of them is 0 where anything else is there.)"""
+    import paper_2410_03960_b200 as P
+    g, x, t = lp_case(10, vocab, dt, vocab)
+    low = torch.finfo(dt).min
+    for i, value in enumerate((low, low / 2, low / 1.7, low / 1.4, low)):
+        x[i, : vocab - 7] = value
+        x[5 + i] = value
+        x[5 + i, (vocab - 1) * i // 4] = 0.5
+    x[0, 9] = -math.inf
+    x[9] = low
+    x[4, : vocab // 2], x[4, vocab // 2:] = 1.0, low
+    t[:5], t[5:] = (torch.tensor([vocab - 1, vocab - 2, vocab - 3, vocab - 4, 0]), torch.tensor([(vocab - 1) * i // 4 for i in range(5)]))
+    got = P.token_logprobs(x, t, temperature=temperature)
+    P.op_status()
+    n = 10
+    if low / temperature < -3.41e38:             # the last row's lse, low / T + log(vocab), is beyond fp32
+        n = 9
+        assert got["lse"][9] == -math.inf and abs(got["entropy"][9] - math.log(vocab)) < 1e-4 and abs(got["logprob"][9] + math.log(vocab)) < 1e-4
+    check_lp(x[:n], t[:n], float(np.float32(temperature)), 0, {k: v[:n] for k, v in got.items()})
+    d = P.token_logprobs_bwd(x, t, got["lse"], got["entropy"], torch.ones(10, device="cuda"), torch.ones(10, device="cuda"), temperature=temperature)
+    assert torch.isfinite(d[:9].float()).all()
+
+
+@pytest.mark.parametrize("dt", [FF, BF, HF])
+@pytest.mark.parametrize("value", [-6e4, -1e6, -1e9, -3e9, -1e10, -1e20, -1e30])
+def test_token_logprobs_masked_by_large_values(dt, value):
+    """The usual constants of masks, over whole chunks ahead of what counts, over a row, and large logits of the other sign."""
+    import paper_2410_03960_b200 as P
+    if dt == HF and value < -65504:
+        value = -65504.0
+    for vocab in (40, 9000, 70000):
+        g, x, t = lp_case(6, vocab, dt, vocab)
+        x[0, : vocab - 9] = value
+        x[1, 3:] = value
+        x[2] = value
+        x[3, vocab // 2] = -value
+        x[4, ::2] = value
+        x[4, 1::2] = -math.inf
+        x[5] = -value
+        t[:] = torch.tensor([vocab - 1, 0, 5, vocab // 2, 4, 7])
+        for temperature in (1.0, 0.6):
+            got = P.token_logprobs(x, t, top_k=3, temperature=temperature)
+            check_lp(x, t, float(np.float32(temperature)), 3, got)
+    P.op_status()
+
+
 def test_token_logprobs_reports_bad_targets():
     import paper_2410_03960_b200 as P
     _, x, t = lp_case(3, 100, BF, 5)
