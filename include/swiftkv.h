@@ -490,13 +490,16 @@ int32_t swiftkv_tail_attention_noalloc(const float *q, const void *k_cache, cons
  * per layer swiftkv_qk_norm_rope (heads normed and rotated, K / V rows stored) and swiftkv_tree_attention (the new tokens
  * against the cache and their own ancestors), at the end swiftkv_token_logprobs.  Like the operators above: DEVICE pointers,
  * queued on `cuda_stream` without synchronising, no allocation; all of them can be captured into a graph.  An index that
- * the device finds outside its range (a target, a position, a cache row, a page, a length beyond the promised maximum) is
- * never followed: the call goes on as stated below and swiftkv_op_status reports SWIFTKV_ERR_BAD_TOKEN.
+ * the device finds outside its range is never followed; the call goes on as stated below.  A target, a position, a slot at or
+ * beyond cache_rows and a length beyond the promised maximum are reported as well, by swiftkv_op_status as SWIFTKV_ERR_BAD_TOKEN.
+ * A page or row outside the cache in what swiftkv_tree_attention is given is not: swiftkv_plan_pages hands out -1 where pages run
+ * short, and says so in `info`.
  */
 
 /* Cache rows of a step's new tokens (pages of SWIFTKV_PAGE_ROWS = 128 rows), planned on the device.
  *   n_past, n_new, n_owned : int32 [n_seqs]; committed tokens, new tokens, entries in use of the sequence's table row (which
- *                 may be more than n_past needs: pages kept after rejected drafts); values below 0 read as 0.  n_seqs <= 8192
+ *                 may be more than n_past needs: pages kept after rejected drafts); values below 0 read as 0, n_owned above
+ *                 max_blocks as max_blocks.  1 <= n_seqs <= 8192
  *   block_table : int32 [n_seqs][max_blocks], page numbers
  *   free_pages  : int32 [free_capacity] with the first *n_free of them free; pages are taken from the end, sequence by sequence
  * Written:
@@ -557,6 +560,11 @@ int32_t swiftkv_qk_norm_rope_bwd(const void *dq, const void *dk, const void *q, 
  * committed token and the new tokens j whose bit is set in its row of tree_mask (bit j % 32 of word j / 32; its own bit is
  * not implied), or, with tree_mask null, those with j <= i.  out = softmax(scale q K^T) V, grouped-query; a token that sees
  * nothing gets zeros and lse = -inf.  What an unseen key's K or V row holds (NaN, infinities) does not matter.
+ * Scores, their maximum and sums, and lse are fp32.  With 16-bit queries a probability is rounded to their type on its way to V (the
+ * sum that divides the result is of the unrounded ones); over an FP8 cache it is a half that carries the V row's scale, and bf16 queries
+ * become halves, each row times a power of two.  fp32 queries: all fp32.  head_dim 64 and 128 with 16-bit queries, 16-byte aligned
+ * planes and token strides and at most 128 query heads per KV head run on the tensor cores, everything else on the CUDA cores: tens of
+ * times slower.
  *   q           : [total_new][n_q_heads][head_dim] in q_dtype (F32, BF16, F16), q_stride elements between tokens
  *   k_cache, v_cache : planes [cache_rows][n_kv_heads][head_dim] of q_dtype, or (kv_dtype SWIFTKV_DTYPE_FP8_E4M3) e4m3 codes with
  *                 k_scale, v_scale fp32 [cache_rows], as swiftkv_kv_cache_view gives them
@@ -564,14 +572,16 @@ int32_t swiftkv_qk_norm_rope_bwd(const void *dq, const void *dk, const void *q, 
  *   row0        : int32 [n_seqs] (position p in row row0[b] + p).  A row outside the cache reads as zeros
  *   n_past int32 [n_seqs], cu_new int32 [n_seqs + 1], tree_mask int32 [total_new][mask_words]
  *   max_new, max_kv : at least the largest number of new tokens and of n_past + new tokens of any sequence; a longer sequence is
- *                 cut there (n_past + new tokens at 2^30 in any case) and reported
+ *                 cut there (n_past + new tokens at 2^30 in any case) and reported.  The layout of the work follows max_new: one near
+ *                 what comes is faster
  *   out         : [total_new][n_q_heads][head_dim] in q_dtype; lse (nullable): fp32 [total_new][n_q_heads], natural logarithm of the
  *                 softmax's denominator.  Rows of tokens that belong to no sequence are left as they were.  out, lse and scratch must not overlap
  *                 q, the cache or one another
  *   softmax_scale : 0 means 1/sqrt(head_dim)
  *   scratch     : >= swiftkv_tree_attention_scratch_bytes(...) bytes (may be null where that is 0), 256-byte aligned, not shared with
  *                 a call that may run at the same time; sufficient for any smaller total_new and max_kv too
- * head_dim <= 256.  Errors: INVALID_ARG, WORKSPACE_SMALL, UNSUPPORTED, CUDA. */
+ * head_dim <= 256.  Errors: INVALID_ARG, WORKSPACE_SMALL, UNSUPPORTED (n_seqs x KV heads x key tiles of max_kv x query tiles of max_new, or
+ * of total_new if that is less, beyond 2^31), CUDA. */
 size_t  swiftkv_tree_attention_scratch_bytes(int32_t total_new, int32_t max_kv, int32_t n_q_heads, int32_t head_dim);
 int32_t swiftkv_tree_attention(const void *q, int64_t q_stride, int32_t q_dtype, const void *k_cache, const void *v_cache,
                                int32_t kv_dtype, const float *k_scale, const float *v_scale, int32_t cache_rows,
@@ -587,7 +597,8 @@ int32_t swiftkv_tree_attention(const void *q, int64_t q_stride, int32_t q_dtype,
  *   top_ids int32 / top_logprobs fp32 [rows][top_k], top_k <= 32: the largest logits in descending order, of equal ones the lowest
  *   index first (0 and -0 are equal; NaN counts as the largest).
  * targets: int32 [rows] or null; a target below 0 gives logprob 0, one at or beyond vocab the same and is reported.  A row
- * without any finite logit has lse -inf and NaN elsewhere; one with a NaN or +inf has NaN.
+ * without any finite logit has lse -inf and NaN elsewhere; one with a NaN or +inf has NaN.  Sums are fp32; exponentials and logarithms
+ * are the GPU's approximate ones (2^-22: results differ from exact ones by about 1e-6 beside the rounding of lse).
  * Errors: INVALID_ARG, CUDA. */
 int32_t swiftkv_token_logprobs(const void *logits, int64_t row_stride, int32_t dtype, const int32_t *targets, int32_t rows,
                                int32_t vocab, float temperature, int32_t top_k, float *logprob, float *entropy, float *lse,

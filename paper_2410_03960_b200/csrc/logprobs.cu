@@ -5,7 +5,7 @@
 //   l = sum 2^(x c - r)      and      s = sum 2^(x c - r) (x c - r)
 // and at the end r = m c with m the largest logit, so that  lse = m / T + ln l,  entropy = (log2 l - s / l) ln 2  (every term of s
 // has one sign: nothing cancels), and  logprob(t) = (x_t - m) / T - ln l.  x c - r is one fused multiply-add, rounded once at its own
-// size; sums are fp32.  r moves only when the sums could grow by more than 2^16.
+// size; sums are fp32.  r moves only when the sums could grow by more than 2^16, and stays within 2^30.
 //
 // Top-k: a bound that at least k logits reach -- after a row's first chunk the k-th largest of the
 // warps' four best thread maxima, later the k-th largest of 32 groups of all threads' maxima so far, which one warp keeps
@@ -17,8 +17,8 @@
 // 16-bit types.  Blocks are persistent and stream rows through a ring of 32 KB bulk copies; a warp of its own joins up a
 // finished row while the others go on with the next.  Few rows: a row is shared by a cluster of up to 8 blocks whose partial
 // results meet in distributed shared memory, so one launch needs no workspace at any size.  Measured at 128256 logits: 4096 rows
-// bf16 with top 5 218 us (4.8 TB/s), 2048 rows fp32 169 us (6.2 TB/s), 33 rows fp32 with top 8 12 us; the gradient of 2048 rows bf16
-// 169 us (6.2 TB/s).
+// bf16 with top 5 226 us (4.7 TB/s), 2048 rows fp32 without top k 157 us (6.7 TB/s), 33 rows fp32 with top 8 12 us; the gradient of 2048
+// rows bf16 169 us (6.2 TB/s).
 #include <cooperative_groups.h>
 
 #include "common.cuh"

@@ -9,7 +9,7 @@
 // Everything after the two prefix sums is independent per table entry and per token: some blocks write the tokens' rows, the others
 // the tables.  The sums run over a few thousand integers at most, so EVERY block computes them for itself (about 1 us for 1024
 // sequences, served by L2) instead of waiting for one that does: a single launch without any communication between blocks.
-// What bounds it: latencies, one after the other (the launch, the lengths, a token's search and page): 3.8 us for 8 sequences,
+// What bounds it: latencies, one after the other (the launch, the lengths, a token's search and page): 3.4 - 3.8 us for 8 sequences,
 // 8.0 us for 1024 sequences with 6.5 MB of tables (their copy alone would take 1 us).
 #include "common.cuh"
 #include "tc_common.cuh"

@@ -14,7 +14,7 @@
 // many blocks as run at once walk over the (token, head) pairs, and what limits them is how many warps' registers fit beside
 // the loads under way.  Other shapes, fp32 and unaligned tensors take the general form (one warp per head, a pair per lane
 // and step).  Measured, 32 + 8 heads of 128, bf16: 16411 tokens 73 us (5.5 TB/s; torch's copy of as many bytes 64 us), 4096
-// tokens into an FP8 cache 27 us; gradient of 8195 tokens 55 us (4.7 TB/s).
+// tokens into an FP8 cache 27 - 29 us; gradient of 8195 tokens 53 us (4.8 TB/s).
 #include "common.cuh"
 #include "tc_common.cuh"
 
@@ -178,7 +178,7 @@ __device__ __forceinline__ void norm_rotate(F2 (&lo)[4], F2 (&hi)[4], bool norm,
 }
 
 // ---- forward, vector form: L lanes per head -----------------------------------------------------------------------------
-// Threads of a block and blocks per SM: registers for one step of loads under way beside one at work, without a spill (16411 tokens
+// Threads of a block and blocks per SM: registers for one step of loads under way beside one at work, 8 bytes of them spilled (16411 tokens
 // of the 8B shape: 73 us; 3 x 256 threads 76, 2 x 256 89, 4 x 256 with a few spilled 79, gains read again from L1 82).  FP8 rows
 // take larger blocks: a row's maximum is taken over one block.
 __host__ __device__ constexpr int rv_threads(bool fp8) { return fp8 ? 256 : 128; }
@@ -378,7 +378,7 @@ constexpr int RB_THREADS = 256;
 constexpr int RB_BLOCKS_PER_SM = 2;      // as many of the vector form as run at once
 // vector form: L lanes per head; the first q_blocks blocks walk over the (token, query head) pairs, the rest over the key heads, the next
 // pair's loads under way while one is computed; gain gradients stay in registers.  These hold it to 16 warps per SM, of 285 instructions
-// a pair and step: 55 us for 8195 tokens of the 8B shape (half as many elements per thread and 24 warps 59, loads by asynchronous
+// a pair and step: 53 us for 8195 tokens of the 8B shape (half as many elements per thread and 24 warps 59, loads by asynchronous
 // copies and two to four steps ahead 59, four times as many blocks 69).
 template <typename T, int L>
 __global__ void __launch_bounds__(RB_THREADS, RB_BLOCKS_PER_SM) qk_norm_rope_bwd_vec_kernel(RopeBwdArgs a, int q_blocks) {

@@ -265,10 +265,12 @@ size_t simt_scratch(int total_new, int max_kv, int n_q, int hd) {
 // leave zeros for the others, and the copies are joined like the pieces of a split key range (in the CTA, through shared memory: 222 us instead of
 // 151 for 24 sequences of 10000 keys).
 //
-// What bounds it: HBM for 16-bit caches and up to about 64 query rows per KV head (24 sequences of one token over 10000 keys 158 us,
+// What bounds it: HBM for 16-bit caches and up to about 64 query rows per KV head (24 sequences of one token over 10000 keys 159 us,
 // 0.96 of the copy bandwidth; 16 of 9 to 32 tokens over 2048 to 8192 keys 70 us, 4.3 TB/s); each stream's chain of softmax, P V and next
-// Q K^T for two full tiles (2 x 64 tokens, 8 heads per KV head, over 131072 keys 470 - 520 us, 1.0 - 1.1 PFLOP/s); shared memory for FP8
-// caches (24 sequences of up to 8 tokens over up to 10000 keys 130 us, 2.8 TB/s); latency for few keys (1 token over 700 keys 11.9 us).
+// Q K^T for two full tiles (2 x 64 tokens, 8 heads per KV head, over 131072 keys 450 - 520 us, 1.0 - 1.2 PFLOP/s); shared memory for FP8
+// caches (24 sequences of up to 8 tokens over up to 10000 keys 130 us, 2.8 TB/s); latency for few keys (1 token over 700 keys 11.7 us).
+// These repeat a call; with the L2 cache emptied between calls: 77, 545, 143 and 12.3 us for the last four.
+// The layouts go by max_new, not by the lengths, which the host does not know: the FP8 case takes 160 us with max_new 16 and 217 with 64.
 //
 // What is not seen must not matter: keys behind the sequence and unseen drafts get S = -inf, and the V rows of the last
 // tiles are cleaned in shared memory first (0 * NaN is NaN): rows behind the sequence become zeros, and so do infinities and NaN in a
@@ -277,7 +279,8 @@ size_t simt_scratch(int total_new, int max_kv, int n_q, int hd) {
 constexpr int TT_KEYS = 128;
 constexpr float TT_RESCALE = 8.0f;       // in log2 units
 // FP8: how far a small V scale (0 for a row outside the cache) draws the reference below the scores.  A key adds at most 2^(80 + TT_RESCALE) to the
-// sum, so 2^30 of them stay below 2^127; rows quantized from zeros (2^-64 / 448) lie above.
+// sum, so 2^30 of them stay below 2^127; rows quantized from zeros (2^-64 / 448) lie above.  (Below 2^-94, where the format has no scale, P
+// falls under the half's normal range.)
 constexpr float TT_LEAST_LOG2 = -80.f;
 
 template <int HD, int W, bool FP8>
