@@ -133,19 +133,21 @@ def test_token_logprobs_of_more_than_32_bits_count(lib, bad):
     assert lib.swiftkv_token_logprobs_bwd(*{**LPB, **bad, "out_stride": 1 << 31}.values()) == INVALID
 
 
-# 5 tokens of 8 + 2 + 2 heads of 128 as slices of one projection's rows (12 heads, 3072 bytes) that start at at(0)
-FUSED = dict(q=at(0), q_stride=1536, k=at(0) + 2048, k_stride=1536, v=at(0) + 2560, v_stride=1536)
+# 5 tokens of 8 + 2 + 2 heads of 128 as slices of one projection's rows (12 heads and 8 elements of padding) that start at at(0)
+WIDE = 12 * 128 + 8
+ROW = 2 * WIDE
+FUSED = dict(q=at(0), q_stride=WIDE, k=at(0) + 2048, k_stride=WIDE, v=at(0) + 2560, v_stride=WIDE)
 
 
-@pytest.mark.parametrize("bad", [dict(q_out=at(0) + 256), dict(q_out=at(0)), dict(q_out=at(0), q_out_stride=1024), dict(q_out=at(0) - 2, q_out_stride=1536),
-                                 dict(q_out=at(0) + 512, q_out_stride=1536), dict(q_out=at(0) + 3072, q_out_stride=2048), dict(k_cache=at(0) + 2048), dict(v_cache=at(0) + 9000),
+@pytest.mark.parametrize("bad", [dict(q_out=at(0) + 256), dict(q_out=at(0)), dict(q_out=at(0), q_out_stride=1024), dict(q_out=at(0) - 2, q_out_stride=WIDE),
+                                 dict(q_out=at(0) + 512, q_out_stride=WIDE), dict(q_out=at(0) + ROW, q_out_stride=2048), dict(k_cache=at(0) + 2048), dict(v_cache=at(0) + 9000),
                                  dict(v_cache=at(7) + 512), dict(q_out=at(8) + 64 * 512 - 2), dict(k_cache=at(0) + 2048, slot_map=None)])
 def test_qk_norm_rope_refuses_overlaps(lib, bad):
     assert lib.swiftkv_qk_norm_rope(*{**ROPE, **FUSED, **bad}.values()) == INVALID
     assert b"overlap" in lib.swiftkv_last_error()
 
 
-@pytest.mark.parametrize("good", [dict(FUSED, q_out=at(0), q_out_stride=1536), dict(FUSED, q_out=at(0) + 4 * 3072 + 3072), dict(FUSED, k_cache=at(0) + 5 * 3072),
+@pytest.mark.parametrize("good", [dict(FUSED, q_out=at(0), q_out_stride=WIDE), dict(FUSED, q_out=at(0) + 5 * ROW), dict(FUSED, k_cache=at(0) + 5 * ROW),
                                   dict(q_out=at(0)), dict(k_cache=at(1), v_cache=at(2), slot_map=None), dict(n_tokens=1, q_out=at(0), q_out_stride=4096)])
 def test_qk_norm_rope_takes_what_shares_no_byte(lib, good):
     """Slices of one projection's rows, results behind their last row, a head on itself: nothing here is refused as an overlap."""
@@ -160,20 +162,20 @@ def test_qk_norm_rope_bwd_refuses_overlaps(lib, bad):
     assert b"overlap" in lib.swiftkv_last_error()
 
 
-@pytest.mark.parametrize("good", [dict(dq_in=at(0), dk_in=at(1)), dict(dq_in=at(2), dk_in=at(3)), dict(dq_in=at(0) + 5 * 2048), dict(q=at(2), q_stride=1536, dk_in=at(2) + 5 * 3072)])
+@pytest.mark.parametrize("good", [dict(dq_in=at(0), dk_in=at(1)), dict(dq_in=at(2), dk_in=at(3)), dict(dq_in=at(0) + 5 * 2048), dict(q=at(2), q_stride=WIDE, dk_in=at(2) + 5 * ROW)])
 def test_qk_norm_rope_bwd_takes_what_shares_no_byte(lib, good):
     if not torch.cuda.is_available():
         assert lib.swiftkv_qk_norm_rope_bwd(*{**BWD, **good}.values()) not in (0, INVALID)
 
 
 @pytest.mark.parametrize("bad", [dict(out=at(0)), dict(out=at(0) + 7 * 2048 + 2046), dict(out=at(1) + 256 * 512 - 2), dict(out=at(2)), dict(lse=at(7)), dict(lse=at(0) + 64),
-                                 dict(q_stride=1536, out=at(0) + 1024), dict(scratch=at(0) - 256), dict(scratch=at(7) - 256), dict(lse=at(8) + 4)])
+                                 dict(q_stride=WIDE, out=at(0) + 1024), dict(scratch=at(0) - 256), dict(scratch=at(7) - 256), dict(lse=at(8) + 4)])
 def test_tree_attention_refuses_overlaps(lib, bad):
     assert lib.swiftkv_tree_attention(*{**TREE, **bad}.values()) == INVALID
     assert b"overlap" in lib.swiftkv_last_error()
 
 
-@pytest.mark.parametrize("good", [dict(out=at(0) + 8 * 2048), dict(q_stride=1536, out=at(0) + 8 * 3072), dict(total_new=1, q_stride=1536, out=at(0) + 2048), dict(lse=at(7) + 8 * 2048)])
+@pytest.mark.parametrize("good", [dict(out=at(0) + 8 * 2048), dict(q_stride=WIDE, out=at(0) + 8 * ROW), dict(total_new=1, q_stride=WIDE, out=at(0) + 2048), dict(lse=at(7) + 8 * 2048)])
 def test_tree_attention_takes_what_shares_no_byte(lib, good):
     if not torch.cuda.is_available():
         assert lib.swiftkv_tree_attention(*{**TREE, **good}.values()) not in (0, INVALID)
