@@ -592,7 +592,7 @@ int32_t swiftkv_tree_attention(const void *q, int64_t q_stride, int32_t q_dtype,
                                void *cuda_stream);
 
 /* Per row of logits [rows][vocab] (F32, BF16 or F16; row_stride elements between rows; rows in [1, 2^26], vocab in [1, 2^30]),
- * z = logits / temperature:
+ * z = logits / temperature, temperature finite and at least 2^-125:
  *   lse = log sum exp z,  logprob = z[target] - lse,  entropy = -sum p log p  (fp32 [rows] each; a logit of -inf adds nothing),
  *   top_ids int32 / top_logprobs fp32 [rows][top_k], top_k <= 32: the largest logits in descending order, of equal ones the lowest
  *   index first (0 and -0 are equal; NaN counts as the largest).

@@ -738,7 +738,8 @@ static int32_t check_logits(const void *logits, int64_t row_stride, int32_t rows
   // (the kernels count a row's elements in 32 bits, in steps of a block's work)
   if (rows < 1 || rows > (1 << 26) || vocab < 1 || vocab > (1 << 30) || row_stride < vocab)
     return report_error(SWIFTKV_ERR_INVALID_ARG, "bad shape (rows in [1, 2^26], vocab in [1, 2^30], row_stride >= vocab)");
-  if (!(temperature > 0.f) || !(temperature < INFINITY)) return report_error(SWIFTKV_ERR_INVALID_ARG, "temperature must be positive and finite");
+  // (below 2^-125 the factor log2(e) / temperature would be infinite, and a row's largest logit 0 times it)
+  if (!(temperature >= 0x1p-125f) || !(temperature < INFINITY)) return report_error(SWIFTKV_ERR_INVALID_ARG, "temperature must be in [2^-125, infinity)");
   if (dtype != SWIFTKV_DTYPE_F32 && dtype != SWIFTKV_DTYPE_BF16 && dtype != SWIFTKV_DTYPE_F16)
     return report_error(SWIFTKV_ERR_INVALID_ARG, "unknown dtype");
   if (reinterpret_cast<uintptr_t>(logits) % (dtype == SWIFTKV_DTYPE_F32 ? 4 : 2)) return report_error(SWIFTKV_ERR_INVALID_ARG, "misaligned logits");

@@ -181,6 +181,12 @@ def test_tree_attention_takes_what_shares_no_byte(lib, good):
         assert lib.swiftkv_tree_attention(*{**TREE, **good}.values()) not in (0, INVALID)
 
 
+def test_token_logprobs_refuses_temperatures_without_a_reciprocal(lib):
+    for t in (1e-45, 1e-40, 2.0 ** -126):
+        assert lib.swiftkv_token_logprobs(*{**LP, "temperature": t}.values()) == INVALID
+        assert lib.swiftkv_token_logprobs_bwd(*{**LPB, "temperature": t}.values()) == INVALID
+
+
 def test_wrappers_refuse_host_tensors(lib):
     import paper_2410_03960_b200 as P
     x, i = torch.zeros(2, 4), torch.zeros(2, dtype=torch.int32)
