@@ -280,7 +280,7 @@ constexpr int TT_KEYS = 128;
 constexpr float TT_RESCALE = 8.0f;       // in log2 units
 // FP8: how far a small V scale (0 for a row outside the cache) draws the reference below the scores.  A key adds at most 2^(80 + TT_RESCALE) to the
 // sum, so 2^30 of them stay below 2^127; rows quantized from zeros (2^-64 / 448) lie above.  (Below 2^-94, where the format has no scale, P
-// falls under the half's normal range.)
+// falls under the half's normal range; and beside a row of scale 0 what has less than about 2^-100 of its probability adds nothing.)
 constexpr float TT_LEAST_LOG2 = -80.f;
 
 template <int HD, int W, bool FP8>
