@@ -693,7 +693,8 @@ int32_t swiftkv_topk_distill(const void *logits, int64_t row_stride, int32_t dty
                              int32_t rows, int32_t vocab, int32_t top_k, double temperature, int32_t rest, float *loss, float *lse,
                              float *rest_lse, const float *grad_loss, void *grad_logits, int64_t grad_stride, void *cuda_stream);
 
-/* The gradient alone, from the lse and rest_lse that the forward call gave. */
+/* The gradient alone, from the lse and rest_lse that the forward call gave.  Where these are so large that fp32 does not resolve them (z / T in the millions), exponents
+ * are off by as much; no q_k and no term of the others' softmax is taken above 1. */
 int32_t swiftkv_topk_distill_bwd(const void *logits, int64_t row_stride, int32_t dtype, const int32_t *top_ids, const float *top_logprobs,
                                  int32_t rows, int32_t vocab, int32_t top_k, double temperature, int32_t rest, const float *lse,
                                  const float *rest_lse, const float *grad_loss, void *grad_logits, int64_t grad_stride,

@@ -81,7 +81,7 @@ struct alignas(16) TdRow {                               // what the two kinds o
   unsigned head, tail;                       // which elements of the row's odd ends are given
   float m, scale;                            // gradient elsewhere: scale 2^((x - m) c)
   TdEntries e;
-  int any;                                   // 0: a row without entries
+  int any;                                   // 0: a row whose others have no gradient (no entries, or the others masked)
   TdPart warp[TD_WARPS];
 };
 struct TdShared {
@@ -520,9 +520,9 @@ __global__ void __launch_bounds__(TD_THREADS + 96, 2) topk_distill_kernel(const 
           if (r.id[k] >= 0) r.grad[k] = (float)((double)g * (r.w[k] * of_w - r.p[k] * of_p) * a.inv_t);
         }
         if (lane == 0) {
-          r.m = o.some ? all.m : 0.f;
-          r.scale = o.some ? (float)((double)g * (o.rest / o.total * (1.0 + off - off_r) - o.p_r) * a.inv_t / (double)all.l * (1.0 + off_r)) : 0.f;
-          r.any = now.any;
+          r.m = all.m;
+          r.scale = (float)((double)g * (o.rest / o.total * (1.0 + off - off_r) - o.p_r) * a.inv_t / (double)all.l * (1.0 + off_r));
+          r.any = now.any && o.some;                       // (others that are masked may be finite and large: an exponential of theirs is not formed)
         }
       }
       __syncwarp();
@@ -619,7 +619,7 @@ __global__ void __launch_bounds__(TD_THREADS + 96, 2) topk_distill_kernel(const 
       T *y = reinterpret_cast<T *>(a.out) + (size_t)row * a.out_stride;
       const int given = tid < a.k ? r.id[tid] : -1;
       wait(&sh.joined[par], (turn / TD_ROWS) & 1);
-      // (a row without entries: as if its logits were 0, whatever they are, times 0)
+      // (nothing for the others: as if their logits were 0, whatever they are, times 0)
       const bool any = r.any != 0;
       const float top = any ? r.m : 0.f, scale = any ? r.scale : 0.f;
       const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
@@ -754,7 +754,9 @@ __global__ void __launch_bounds__(TB_THREADS) topk_distill_bwd_kernel(TdBwdArgs 
   const double p_r = a.rest && some ? fmax(1.0 - all_p, 0.0) : 0.0, norm = a.rest || !(all_p > 0.0) ? 1.0 : all_p;
   const float scale = some ? (float)((double)g * (exp((double)rest_lse - (double)lse) - p_r) * a.inv_t) : 0.f;
   const float c = (float)(1.4426950408889634 * a.inv_t), ref = some ? (float)(1.4426950408889634 * (double)rest_lse) : 0.f;
-  auto slope = [&](float v) { return any ? scale * exp2_approx(fmaf(v, c, -ref)) : 0.f; };      // (a row without entries: 0, whatever its logits are)
+  // No term of a softmax is above 1, whatever the rounding of a large rest_lse leaves; nor, with a scale of 0, one of masked others that are finite and large.  (A
+  // row without entries: 0, whatever its logits are.)
+  auto slope = [&](float v) { return any ? scale * exp2_approx(fminf(fmaf(v, c, -ref), 0.f)) : 0.f; };
   if (part == 0 && tid < head) lp_store(y + tid, slope(lp_load(x + tid)));
   if (part == b.blocks_per_row - 1 && tail0 + tid < a.vocab) lp_store(y + tail0 + tid, slope(lp_load(x + tail0 + tid)));
   for (int v0 = v_begin + tid; v0 - lane < v_end; v0 += TB_THREADS * UNROLL) {      // (the warp's lanes stay together)
@@ -777,7 +779,10 @@ __global__ void __launch_bounds__(TB_THREADS) topk_distill_bwd_kernel(TdBwdArgs 
     }
   }
   __syncthreads();
-  if (id >= e0 && id < e1) lp_store(y + id, (float)((double)g * (exp((double)z * a.inv_t + td_rounding(z, a.inv_t) - (double)lse) - p / norm) * a.inv_t));
+  if (id >= e0 && id < e1) {
+    const double t = (double)z * a.inv_t + td_rounding(z, a.inv_t) - (double)lse;
+    lp_store(y + id, (float)((double)g * (exp(t > 0.0 ? 0.0 : t) - p / norm) * a.inv_t));      // (likewise; NaN stays)
+  }
 }
 
 template <typename T, bool GRAD>
