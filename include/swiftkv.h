@@ -684,17 +684,18 @@ int32_t swiftkv_commit_drafts(void *const *planes, const int64_t *row_bytes, int
  * p_k = 0 adds nothing; a logit of -inf at p_k > 0 gives +inf; NaN or +inf among the logits, or no finite one, gives NaN.  T in [2^-64, 2^100].
  * grad_logits (nullable; `dtype`, grad_stride elements between rows, may be the logits themselves: same pointer and stride): the gradient of
  * sum grad_loss[row] loss[row] with respect to the logits, grad_loss fp32 [rows] (given exactly where grad_logits is),
- *   grad_loss (q_k - p_k) / T  at the entries,   grad_loss (q_r - p_r) exp(z - rest_lse) / T  elsewhere,
- * with q_k = exp(z_k - lse), q_r = exp(rest_lse - lse) of z_k as the fp32 product of logit and 1 / T and of the log sums as they are returned (where
- * they are below 64), from one pass over HBM: the second look at a row is served by the L2 cache.  Sums over the other tokens are fp32, with the
+ *   grad_loss (P q_k - p_k) / T  at the entries,   grad_loss (P q_r - p_r) exp(z - rest_lse) / T  elsewhere,   P = sum p_k + p_r
+ * (1, but where sum p_k > 1 by more than 2^-17, what rounded log probabilities may be off by; where the others are masked; and where no p_k is above 0 at
+ * rest == 0), with q_k = exp(z_k - lse), q_r = exp(rest_lse - lse) of z_k as the fp32 product of logit and 1 / T and of the log sums as they are returned
+ * (where they are below 64), from one pass over HBM: the second look at a row is served by the L2 cache.  Sums over the other tokens are fp32, with the
  * GPU's approximate exponentials (2^-22); what is formed of them and the entries is 64-bit.  Repeats bit for bit.
  * rows <= 2^26, vocab <= 2^30.  Errors: INVALID_ARG, CUDA. */
 int32_t swiftkv_topk_distill(const void *logits, int64_t row_stride, int32_t dtype, const int32_t *top_ids, const float *top_logprobs,
                              int32_t rows, int32_t vocab, int32_t top_k, double temperature, int32_t rest, float *loss, float *lse,
                              float *rest_lse, const float *grad_loss, void *grad_logits, int64_t grad_stride, void *cuda_stream);
 
-/* The gradient alone, from the lse and rest_lse that the forward call gave.  Where these are so large that fp32 does not resolve them (z / T in the millions), exponents
- * are off by as much; no q_k and no term of the others' softmax is taken above 1. */
+/* The gradient alone, from the lse and rest_lse that the forward call gave.  Where these are so large that fp32 does not resolve them (z / T beyond 10^5), exponents
+ * are off by as much, those of the others to the lower side: no q_k and no term of the others' softmax comes out above 1. */
 int32_t swiftkv_topk_distill_bwd(const void *logits, int64_t row_stride, int32_t dtype, const int32_t *top_ids, const float *top_logprobs,
                                  int32_t rows, int32_t vocab, int32_t top_k, double temperature, int32_t rest, const float *lse,
                                  const float *rest_lse, const float *grad_loss, void *grad_logits, int64_t grad_stride,

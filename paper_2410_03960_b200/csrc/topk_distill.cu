@@ -1,9 +1,10 @@
 // swiftkv_topk_distill: the divergence of a student's distribution from a teacher's largest log probabilities, and its gradient with respect
 // to the student's logits; swiftkv_topk_distill_bwd: the gradient alone.
 //
-// With the K given tokens and all others as one outcome, q_k = e^(z_k - lse), q_r = e^(lse_r - lse) (lse_r over the others), the
-// gradient is g (q_k - p_k) / T at the given tokens and g (q_r - p_r) / T times the others' own softmax e^(z - lse_r) elsewhere -- a
-// factor of at most 1 and a softmax, so nothing overflows where the others have hardly any probability.  For the same reason the others
+// With the K given tokens and all others as one outcome, q_k = e^(z_k - lse), q_r = e^(lse_r - lse) (lse_r over the others) and the mass P = sum p_k + p_r,
+// the gradient is g (P q_k - p_k) / T at the given tokens and g (P q_r - p_r) / T times the others' own softmax e^(z - lse_r) elsewhere -- a
+// factor of at most P and a softmax, so nothing overflows where the others have hardly any probability.  P is 1 but where p_r is cut off at 0 or counts as 0, or
+// nothing has any probability.  For the same reason the others
 // are summed apart: taking the given tokens' exponentials off a sum over everything would leave rounding.  Given tokens are
 // blanked in shared memory before a chunk is summed.  What is formed of the K + 1 outcomes is 64-bit: the loss is a small difference of
 // logarithms, and p_r = 1 - sum p loses its bits where the teacher is sure.  An error of the others' sum itself enters the loss by
@@ -66,6 +67,11 @@ __device__ __forceinline__ double td_rounding(float z, double inv_t) {
   return fabs(exact) < 64.0 ? (double)(z * (float)inv_t) - exact : 0.0;
 }
 __device__ __forceinline__ double td_rounding(double x) { return fabs(x) < 64.0 ? (double)(float)x - x : 0.0; }
+
+// The mass P = sum p_k + p_r of entries with the sum p: p_r makes it 1 where there are others for it and p leaves it something, dividing by p where that is not 0
+// (a NaN stays).  Log probabilities in fp32 of logits up to 64 are off by 2 x 2^-18, and so is their sum where the teacher is sure: that near to 1 it is 1.  (Of 7500
+// drawn fp32 batches two, of one and two rows, had gradients 6e-5 and 3e-4 off without this, in the 2-norm; the others are the same.)
+__device__ __forceinline__ double td_mass(double p, int rest, bool some) { return (rest ? (some && p <= 1.0) || fabs(p - 1.0) <= 0x1p-17 : p > 0.0) ? 1.0 : p; }
 
 struct TdPart { float m, l; };               // a set of logits: its maximum, and the sum of 2^((x - m) c)
 // One warp's sums over a row's entries: their largest logit (-inf: none), weights relative to it, the teacher's probabilities, sum p (log p - z / T)
@@ -280,6 +286,7 @@ struct TdOutcome {
   float top;               // the row's largest logit
   double total, rest;      // sum of weights relative to it, and the others'
   double p_r, norm;        // the others' probability, and what the entries' are divided by
+  double mass;             // what all outcomes' then sum to
   double f;                // the entries' weights are relative to their own largest: times this
   bool some;               // there are others that are not masked
 };
@@ -298,6 +305,7 @@ __device__ __forceinline__ TdOutcome td_outcome(const TdEntries &e, const TdPart
   o.some = !none && !(o.rest < o.total * TD_MASKED);
   o.p_r = a.rest && o.some ? fmax(1.0 - e.p, 0.0) : 0.0;
   o.norm = a.rest || !(e.p > 0.0) ? 1.0 : e.p;
+  o.mass = td_mass(e.p, a.rest, o.some);
   return o;
 }
 
@@ -513,7 +521,7 @@ __global__ void __launch_bounds__(TD_THREADS + 96, 2) topk_distill_kernel(const 
       const double rest_lse = all.m == -INFINITY ? -INFINITY : (double)all.m * a.inv_t + __shfl_sync(0xffffffffu, log_x, 1);
       if (GRAD) {
         const double off = -td_rounding(lse), off_r = -td_rounding(rest_lse);      // (so small that 1 + off is e^off)
-        const double of_w = o.f / o.total * (1.0 + off), of_p = 1.0 / o.norm;
+        const double of_w = o.mass * o.f / o.total * (1.0 + off), of_p = 1.0 / o.norm;
 #pragma unroll
         for (int i = 0; i < TD_LANE_TOP; ++i) {
           const int k = i * 32 + lane;
@@ -521,7 +529,7 @@ __global__ void __launch_bounds__(TD_THREADS + 96, 2) topk_distill_kernel(const 
         }
         if (lane == 0) {
           r.m = all.m;
-          r.scale = (float)((double)g * (o.rest / o.total * (1.0 + off - off_r) - o.p_r) * a.inv_t / (double)all.l * (1.0 + off_r));
+          r.scale = (float)((double)g * (o.mass * o.rest / o.total * (1.0 + off - off_r) - o.p_r) * a.inv_t / (double)all.l * (1.0 + off_r));
           r.any = now.any && o.some;                       // (others that are masked may be finite and large: an exponential of theirs is not formed)
         }
       }
@@ -694,6 +702,7 @@ __global__ void __launch_bounds__(TB_THREADS) topk_distill_bwd_kernel(TdBwdArgs 
   constexpr int N = LpVec<T>::N, UNROLL = EVEN ? TB_UNROLL : TB_UNROLL / 2;
   __shared__ int s_id[TD_MAX_TOP];
   __shared__ double s_p[TD_MAX_TOP / 32];
+  __shared__ double s_mass;                                // (a register that the vectors need)
   const TdArgs &a = b.a;
   const int tid = threadIdx.x, lane = tid & 31;
   const int row = blockIdx.x / b.blocks_per_row, part = blockIdx.x % b.blocks_per_row;
@@ -751,12 +760,14 @@ __global__ void __launch_bounds__(TB_THREADS) topk_distill_bwd_kernel(TdBwdArgs 
 #pragma unroll
   for (int w = 0; w < TD_MAX_TOP / 32; ++w) all_p += s_p[w];
   const bool some = rest_lse != -INFINITY && !((double)rest_lse < (double)lse - TD_MASKED_LOG);      // (a NaN counts)
-  const double p_r = a.rest && some ? fmax(1.0 - all_p, 0.0) : 0.0, norm = a.rest || !(all_p > 0.0) ? 1.0 : all_p;
-  const float scale = some ? (float)((double)g * (exp((double)rest_lse - (double)lse) - p_r) * a.inv_t) : 0.f;
-  const float c = (float)(1.4426950408889634 * a.inv_t), ref = some ? (float)(1.4426950408889634 * (double)rest_lse) : 0.f;
-  // No term of a softmax is above 1, whatever the rounding of a large rest_lse leaves; nor, with a scale of 0, one of masked others that are finite and large.  (A
-  // row without entries: 0, whatever its logits are.)
-  auto slope = [&](float v) { return any ? scale * exp2_approx(fminf(fmaf(v, c, -ref), 0.f)) : 0.f; };
+  const double p_r = a.rest && some ? fmax(1.0 - all_p, 0.0) : 0.0, norm = a.rest || !(all_p > 0.0) ? 1.0 : all_p, mass = td_mass(all_p, a.rest, some);
+  if (tid == 0) s_mass = mass;
+  const float scale = some ? (float)((double)g * (mass * exp((double)rest_lse - (double)lse) - p_r) * a.inv_t) : 0.f;
+  const float c = (float)(1.4426950408889634 * a.inv_t);
+  // No term of a softmax is above 1: a reference that does not resolve that (2^18: exponents off by 3 x 2^-6) is raised by what rest_lse, it and c may be rounded by
+  const float near_ref = (float)(1.4426950408889634 * (double)rest_lse), ref = fabsf(near_ref) > 0x1p18f ? near_ref + fabsf(near_ref) * 0x1p-22f : near_ref;
+  const bool sloped = any && some;                         // (no entries, or others that are masked, be they finite and large: 0)
+  auto slope = [&](float v) { return sloped ? scale * exp2_approx(fmaf(v, c, -ref)) : 0.f; };
   if (part == 0 && tid < head) lp_store(y + tid, slope(lp_load(x + tid)));
   if (part == b.blocks_per_row - 1 && tail0 + tid < a.vocab) lp_store(y + tail0 + tid, slope(lp_load(x + tail0 + tid)));
   for (int v0 = v_begin + tid; v0 - lane < v_end; v0 += TB_THREADS * UNROLL) {      // (the warp's lanes stay together)
@@ -781,7 +792,8 @@ __global__ void __launch_bounds__(TB_THREADS) topk_distill_bwd_kernel(TdBwdArgs 
   __syncthreads();
   if (id >= e0 && id < e1) {
     const double t = (double)z * a.inv_t + td_rounding(z, a.inv_t) - (double)lse;
-    lp_store(y + id, (float)((double)g * (exp(t > 0.0 ? 0.0 : t) - p / norm) * a.inv_t));      // (likewise; NaN stays)
+    const bool above = __double2hiint(t) >= 0x3f900000 && __double2hiint(t) <= 0x7ff00000;      // (2^-6 to infinity: likewise)
+    lp_store(y + id, (float)((double)g * (s_mass * exp(above ? 0.0 : t) - p / norm) * a.inv_t));
   }
 }
 

@@ -1,9 +1,11 @@
 """verify_drafts, commit_drafts, topk_distill and its gradient on the GPU in calls that the documentation allows and ordinary inputs do not make: against
-64-bit restatements (draft_reference.py).  Bounds are those of test_gpu_drafts.py, where they are derived."""
+64-bit restatements (draft_reference.py, distill_slope.py).  Bounds are those of test_gpu_drafts.py, where they are derived."""
 import numpy as np
 import pytest
 import torch
 
+import distill_slope as S
+import draft_reference as R
 import test_gpu_drafts as T
 from test_gpu_drafts import BF, D, FF, HF, f32, f64, i32, u_of
 
@@ -50,3 +52,84 @@ def test_topk_distill_gradient_alone_stays_a_softmax_where_log_sums_are_coarse(d
     for grad in (got["grad_logits"], alone):
         assert (grad.double().abs() <= (weight.double().abs() / temp)[:, None] * (1 + u_of(dt) + 1e-6)).all()
     P.op_status()
+
+
+def special(dt, rows, vocab, kind, seed=31):
+    """Rows whose teacher's outcomes do not sum to one, every second row; ordinary ones between them."""
+    z, ids, lp, weight = T.teacher(seed, rows, vocab, 4, dt, 1.0, sharp=1.5)
+    z, lp, odd = z.clone(), lp.clone(), torch.arange(rows, device="cuda") % 2 == 0
+    if kind == "others masked":
+        keep = torch.zeros((rows, vocab), dtype=torch.bool, device="cuda").scatter_(1, ids.long(), True)
+        z[odd[:, None] & ~keep] = -float("inf")
+        lp[odd] = torch.log(f32([0.4, 0.3, 0.06, 0.04]))
+    elif kind == "above one":
+        lp[odd] = torch.log(f32([0.5, 0.4, 0.1, 0.02]))
+    elif kind == "nothing":
+        lp[odd] = -float("inf")
+    elif kind == "whole vocabulary":                       # (vocab = 4: there are no others)
+        lp[odd] = torch.log(f32([0.4, 0.3, 0.06, 0.04]))
+    return z, ids, lp, weight
+
+
+@pytest.mark.parametrize("dt", [FF, BF, HF])
+@pytest.mark.parametrize("rows,vocab,kind", [(r, v, k) for r, v in ((6, 40), (5, 4097), (3, 40000), (320, 2001)) for k in ("others masked", "above one", "nothing")] + [(6, 4, "whole vocabulary")])
+@pytest.mark.parametrize("temp,rest", [(1.0, True), (1.0, False), (0.7, True), (3.0, True)])
+def test_topk_distill_gradient_where_the_teacher_does_not_sum_to_one(dt, rows, vocab, kind, temp, rest):
+    """The slope of the returned loss: P q - p with P = sum p + p_r.  An error d of lse changes P q_k by P q_k d; elsewhere (P q_r - p_r) s, with s the others'
+    softmax, by P q_r s d and, through s, by |P q_r - p_r| 2 d; the gradient alone has rounded log sums and exponents beside."""
+    import paper_2410_03960_b200 as P
+    z, ids, lp, weight = special(dt, rows, vocab, kind)
+    kept, g, ids_h = f64(z), f64(weight), ids.cpu().numpy()
+    loss, lse, rest_lse, y, qr, pr = S.distill(kept, ids_h, f64(lp), temp, rest, g)
+    mass = S.masses(kept, ids_h, f64(lp), temp, rest)
+    got = P.topk_distill(z, ids, lp, temperature=temp, rest=rest, grad_loss=weight)
+    alone = P.topk_distill_bwd(z, ids, lp, got["lse"], got["rest_lse"], weight, temperature=temp, rest=rest)
+    given = np.zeros(kept.shape, bool)
+    np.put_along_axis(given, ids_h.astype(np.int64), True, 1)
+    with np.errstate(invalid="ignore"):
+        s = np.nan_to_num(np.exp(np.minimum(kept / temp - np.where(np.isfinite(rest_lse), rest_lse, np.inf)[:, None], 0.0)))
+    q = np.exp(kept / temp - lse[:, None])
+    size = np.abs(np.where(np.isfinite(kept), kept, 0.0)) / temp + np.abs(np.where(np.isfinite(rest_lse), rest_lse, 0.0))[:, None] + np.abs(lse)[:, None]
+    inv = (np.abs(g) / temp)[:, None]
+    for x, more in ((got["grad_logits"], 0.0), (alone, 1.0)):
+        off = np.where(given, mass[:, None] * q, s * (mass * qr + 2 * np.abs(mass * qr - pr))[:, None]) * inv * (D * (1 + more) + more * 4 * size * 2.0 ** -24)
+        assert (np.abs(f64(x) - y) <= off + u_of(dt) * (np.abs(y) + off) + (2.0 ** -25 if dt == HF else 1e-37)).all(), np.abs(f64(x) - y).max()
+    assert (np.abs(f64(got["loss"]) - loss) <= (np.abs(mass * qr - pr) + D) * D + 2.0 ** -24 * np.abs(loss) + 1e-12).all()
+    P.op_status()
+
+
+@pytest.mark.parametrize("kind", ["others masked", "above one", "nothing"])
+@pytest.mark.parametrize("rest", [True, False])
+def test_topk_distill_gradient_against_differences_where_the_teacher_does_not_sum_to_one(kind, rest):
+    """Central differences of the 64-bit loss, as in test_gpu_drafts.py; and both calls."""
+    import paper_2410_03960_b200 as P
+    z, ids, lp, weight = special(FF, 4, 40, kind, 32)
+    got = P.topk_distill(z, ids, lp, temperature=1.3, rest=rest, grad_loss=weight)
+    alone = P.topk_distill_bwd(z, ids, lp, got["lse"], got["rest_lse"], weight, temperature=1.3, rest=rest)
+    x, h = f64(z), 1e-4
+    loss = lambda a: R.distill(a, ids.cpu().numpy(), f64(lp), 1.3, rest)[0]  # noqa: E731
+    for v in range(40):
+        up, down = x.copy(), x.copy()
+        up[:, v] += h
+        down[:, v] -= h
+        with np.errstate(invalid="ignore"):
+            want = (loss(up) - loss(down)) / (2 * h) * f64(weight)
+        for grad in (got["grad_logits"], alone):
+            assert (np.abs(f64(grad)[:, v] - want) <= (h * h + 1e-11 + 2 * D) * np.abs(f64(weight))).all(), v
+
+
+@pytest.mark.parametrize("dt", [FF, BF])
+@pytest.mark.parametrize("vocab,rows", [(6, 6), (700, 6), (40000, 6), (3000, 320)])
+@pytest.mark.parametrize("rest", [True, False])
+def test_topk_distill_entries_that_are_missing_or_double(monkeypatch, dt, vocab, rows, rest):
+    """The rows of the test of that name in test_gpu_drafts.py, with the loss's own slope."""
+    monkeypatch.setattr(R, "distill", S.distill)
+    T.test_topk_distill_entries_that_are_missing_or_double(dt, vocab, rows, rest)
+
+
+@pytest.mark.parametrize("dt", [FF, BF, HF])
+@pytest.mark.parametrize("vocab", [12, 3001, 50000])
+def test_topk_distill_masked_logits(monkeypatch, dt, vocab):
+    """Likewise."""
+    monkeypatch.setattr(R, "distill", S.distill)
+    T.test_topk_distill_masked_logits(dt, vocab)
