@@ -316,7 +316,9 @@ __device__ __forceinline__ VdStretch vd_stretch(const double *x, int n) {
   return s;
 }
 // all warps of the block that has it: the first token of the block's part at which the sum of the weights exceeds target (the last that has a weight where
-// rounding leaves none); true in the thread that found it
+// rounding leaves none); true in the one thread that found it.  Sums of the same numbers differ by how they are taken together, so each choice -- tile, step, lane,
+// element -- is made among candidates that have a weight and does not lean on the choice before it: what lies before a tile counts as at most target, and the step
+// is the one whose own two ends, each formed once, enclose it.
 template <typename T>
 __device__ __forceinline__ bool vd_find(VdShared &sh, const int *tried, const VdRow<T> &r, double target, int &token) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -325,7 +327,7 @@ __device__ __forceinline__ bool vd_find(VdShared &sh, const int *tried, const Vd
     const unsigned over = __ballot_sync(0xffffffffu, s.sum > 0.0 && s.until > target), some = __ballot_sync(0xffffffffu, s.sum > 0.0);
     const int who = over ? __ffs(over) - 1 : 31 - __clz(some | 1u);
     if (lane == who) {
-      double sum = s.until - s.sum, before = sum;
+      double sum = fmin(s.until - s.sum, target), before = sum;
       int tile = 0;
       for (int i = s.i0; i < s.i1; ++i) {
         const double w = sh.tile[i];
@@ -363,6 +365,7 @@ __device__ __forceinline__ bool vd_find(VdShared &sh, const int *tried, const Vd
     __syncthreads();
     double base = before;
     for (int i = 0; i < warp; ++i) base += sh.step_sum[i];
+    const bool here = !(base > target) && base + sh.step_sum[warp] > target;
     const unsigned over = __ballot_sync(0xffffffffu, sum > 0.0 && base + until > target), some = __ballot_sync(0xffffffffu, sum > 0.0);
     const int who = over ? __ffs(over) - 1 : 31 - __clz(some | 1u);
     if (some && lane == who) {
@@ -374,10 +377,10 @@ __device__ __forceinline__ bool vd_find(VdShared &sh, const int *tried, const Vd
         at += w[i];
         if (w[i] > 0.0) e = r.element(v, i);
       }
-      if (over && !(base > target)) {
+      if (here) {
         token = e;
         found = true;
-      } else if (!over) {
+      } else {
         atomicMax(&sh.last, e);
       }
     }

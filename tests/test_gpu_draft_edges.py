@@ -133,3 +133,42 @@ def test_topk_distill_masked_logits(monkeypatch, dt, vocab):
     """Likewise."""
     monkeypatch.setattr(R, "distill", S.distill)
     T.test_topk_distill_masked_logits(dt, vocab)
+
+
+# ---------------------------------------------------------------------------------------------------- verify_drafts
+@pytest.mark.parametrize("dt", [FF, BF])
+@pytest.mark.parametrize("n_seqs,vocab", [(1500, 1024), (1500, 2048), (40, 8192), (4, 70000)])
+@pytest.mark.parametrize("repeats,holes", [(2, False), (4, False), (4, True)])
+@pytest.mark.parametrize("probs", [False, True])
+def test_verify_drafts_draws_at_a_border_between_tiles(dt, n_seqs, vocab, repeats, holes, probs):
+    """Rows that repeat themselves, and random numbers at the borders between the repetitions, where sums that are rounded in another order lie on either side: somebody
+    writes a token, and it is one whose prefix sums enclose the target.  (Weights are good to 1e-14 and at most vocab sums to 2^-53 each: 1e-11 covers both.)"""
+    import paper_2410_03960_b200 as P
+    g = torch.Generator(device="cuda").manual_seed(vocab + repeats)
+    part = torch.randn((n_seqs, vocab // repeats), generator=g, device="cuda") * 2
+    if holes:                                              # most tokens are masked: whole lanes have no weight
+        part[torch.rand(part.shape, generator=g, device="cuda") < 0.95] = -float("inf")
+        part[:, 0] = 1.0
+    row = part.to(dt).repeat(1, repeats)
+    news = 2 if probs else 1
+    z = row.repeat_interleave(news, 0)
+    places = torch.arange(n_seqs, device="cuda") % (repeats - 1) + 1
+    u = torch.full((n_seqs, news), 0.99999, device="cuda")
+    u[:, 0] = places / repeats
+    q = None
+    left = torch.softmax(row.double(), 1)
+    if probs:                                              # the drafted token falls: what it was given goes off the row, the same in every repetition
+        q = torch.zeros((news * n_seqs, vocab), device="cuda")
+        q[1::2, torch.arange(repeats, device="cuda") * (vocab // repeats)] = 1.0 / repeats
+        left = (left - q[1::2].double()).clamp(min=0.0)
+    out = {k: torch.full((n_seqs, news) if k != "n_accepted" else (n_seqs,), -77, dtype=torch.int32, device="cuda") for k in ("n_accepted", "tokens", "path")}
+    tokens = torch.zeros(news * n_seqs, dtype=torch.int32, device="cuda")
+    P.verify_drafts(z, tokens, i32(news * np.arange(n_seqs + 1)), news, u.flatten(), draft_probs=q, out=out)
+    assert (out["n_accepted"] == 0).all()
+    token = out["tokens"][:, 0].long()
+    assert ((token >= 0) & (token < vocab)).all()
+    sums = left.cumsum(1)
+    total, target = sums[:, -1], u[:, 0].double() * sums[:, -1]
+    until, weight = sums.gather(1, token[:, None])[:, 0], left.gather(1, token[:, None])[:, 0]
+    assert (weight > 0).all() and (until >= target - 1e-11 * total).all() and (until - weight <= target + 1e-11 * total).all()
+    P.op_status()
