@@ -631,15 +631,16 @@ int32_t swiftkv_token_logprobs_bwd(const void *logits, int64_t row_stride, int32
  *   with draft_probs    : token c stands if  uniforms[c] q_c S < w_c,  q = draft_probs[c], the distribution that c was drawn from
  *   T = 0               : token c stands if it is the largest logit's, of equal ones the lowest index
  * The first that stands becomes x; where none does, the next token v is the first with  sum_{i <= v} r_i > uniforms[cu_new[b]] sum r,  where
- * r = w without the fallen tokens, or max(w - S q, 0) with the fallen token's q, or w where none fell (or nothing of r is left);
+ * r = w without the fallen tokens, or max(w - S q, 0) with the fallen token's q, or w where none fell (or nothing of r is left; an id outside [0, vocab)
+ * does not count as fallen);
  * T = 0: the largest logit's.  With uniforms from [0, 1) the tokens are distributed as the target's.
  *   logits      : [total_new][vocab] in `dtype` (F32, BF16, F16), row_stride elements between rows
  *   tokens      : int32 [total_new], the new tokens' ids (a sequence's first entry is not looked at); an id outside [0, vocab) never stands
  *                 (at or beyond vocab: reported)
  *   parents     : int32 [total_new], parent's place in the sequence, below the token's own (others: the token is never reached, and reported;
  *                 a sequence's first entry is not looked at).  Null: every token's parent is the one before it
- *   draft_probs : fp32 [total_new][vocab], draft_stride elements between rows (a sequence's first row is not looked at; values below 0 and NaN count as
- *                 0), or null: the drafter chose for certain.  Chains only: not together with parents
+ *   draft_probs : fp32 [total_new][vocab], draft_stride elements between rows (a sequence's first row and those of ids outside [0, vocab) are not looked at; values below 0
+ *                 and NaN count as 0), or null: the drafter chose for certain.  Chains only: not together with parents
  *   uniforms    : fp32 [total_new]; below 0 and NaN count as 0, 1 and above as the largest number below 1.  May be null where `temperatures` is
  *                 and temperature is 0
  *   temperatures: fp32 [n_seqs], or null: `temperature` for all.  0, or in [2^-64, 2^100]; anything else on the device counts as 0 and is

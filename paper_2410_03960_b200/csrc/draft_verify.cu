@@ -550,7 +550,9 @@ __global__ void __launch_bounds__(VD_THREADS, 2) verify_drafts_kernel(const __gr
     }
     d.token[j] = token;
     d.tried[j] = p;                                    // (the parents, until the walk begins)
-    d.first[j] = a.parents ? NO_CHILD : j + 1;
+    // a chain ends in front of an id that is none: it cannot stand, and nothing was drawn from its row of probabilities, which therefore does not go off the target
+    if (a.parents || j == n - 1) d.first[j] = NO_CHILD;
+    if (!a.parents && j > 0) d.first[j - 1] = token >= 0 && token < a.vocab ? j : NO_CHILD;
     d.next[j] = NO_CHILD;
     if (part == 0 && j > 0 && token >= a.vocab) atomicOr(a.status, STATUS_BAD_TOKEN);
     if (!greedy) {

@@ -172,3 +172,29 @@ def test_verify_drafts_draws_at_a_border_between_tiles(dt, n_seqs, vocab, repeat
     until, weight = sums.gather(1, token[:, None])[:, 0], left.gather(1, token[:, None])[:, 0]
     assert (weight > 0).all() and (until >= target - 1e-11 * total).all() and (until - weight <= target + 1e-11 * total).all()
     P.op_status()
+
+
+@pytest.mark.parametrize("dt", [FF, BF])
+@pytest.mark.parametrize("news,vocab", [([2] * 8, 4), ([5] * 40, 1000), ([6, 1, 8, 3], 40001), ([4] * 300, 5003)])
+def test_verify_drafts_ids_that_are_none_with_the_drafters_probabilities(dt, news, vocab):
+    """A shorter draft padded with -1, ids at or beyond the vocabulary, at several depths: nothing was drawn from such a row of draft_probs, whatever it holds, and nothing
+    of it goes off the target."""
+    import paper_2410_03960_b200 as P
+    z, tokens, cu, _, q, u = T.drafts(vocab, news, vocab, dt, probs=True)
+    junk = [0.0, float("nan"), float("inf"), 1.0, -1.0]
+    for b, n in enumerate(news):
+        if n < 2:
+            continue
+        j = 1 + b % (n - 1)
+        tokens[cu[b] + j:cu[b] + n] = -1
+        q[cu[b] + j:cu[b] + n] = junk[b % 5]
+    for temps in (None, np.random.default_rng(1).choice([1.0, 0.0, 0.5], len(news))):
+        T.check_verify(z, tokens, cu, None, q, u, temps)
+    P.op_status()
+    tokens[tokens == -1] = vocab
+    T.check_verify(z, tokens, cu, None, q, u)
+    with pytest.raises(P.SwiftKVError):
+        P.op_status()
+    z = torch.zeros((2, 4), dtype=dt, device="cuda")
+    q = f32([[0, 0, 0, 0], [1, 0, 0, 0]])
+    assert P.verify_drafts(z, i32([0, -1]), i32([0, 2]), 2, f32([0, 0]), draft_probs=q)["tokens"].tolist() == [[0, -1]]
