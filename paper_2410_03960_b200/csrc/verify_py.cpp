@@ -11,6 +11,7 @@
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <limits>
 #include <optional>
 #include <sstream>
 #include <stdexcept>
@@ -384,7 +385,11 @@ PyObject *verify_drafts(PyObject *, PyObject *const *a, Py_ssize_t argc) {
     }
     float *p_temps = nullptr, temperature = 1.f;
     if (THPVariable_Check(a[7])) p_temps = floats(on, a[7], "temperature", n);
-    else temperature = f32(a[7]);
+    else {
+      const double given = f64(a[7]);
+      temperature = (float)given;
+      if (temperature == 0.f && given != 0.0) temperature = std::numeric_limits<float>::quiet_NaN();      // (not the 0 of a greedy choice: refused with all else out of range)
+    }
     int32_t *p_n = ints(on, a[8], "out n_accepted", n);
     int32_t *p_out = static_cast<int32_t *>(whole(on, tensor(a[9], "out tokens"), "out tokens", {n, max_new}, at::kInt));
     int32_t *p_path = static_cast<int32_t *>(whole(on, tensor(a[10], "out path"), "out path", {n, max_new}, at::kInt));

@@ -198,3 +198,15 @@ def test_verify_drafts_ids_that_are_none_with_the_drafters_probabilities(dt, new
     z = torch.zeros((2, 4), dtype=dt, device="cuda")
     q = f32([[0, 0, 0, 0], [1, 0, 0, 0]])
     assert P.verify_drafts(z, i32([0, -1]), i32([0, 2]), 2, f32([0, 0]), draft_probs=q)["tokens"].tolist() == [[0, -1]]
+
+
+def test_verify_drafts_refuses_temperatures_that_32_bits_round_to_0():
+    import paper_2410_03960_b200 as P
+    z, args = torch.randn((2, 50), device="cuda"), (i32([0, 1]), i32([0, 2]), 2, f32([0.5, 0.5]))
+    for t in (1e-50, -1e-50, 5e-324, 1e-46, 1e39, -1e39):
+        with pytest.raises(P.SwiftKVError) as e:
+            P.verify_drafts(z, *args, temperature=t)
+        assert e.value.code == -1
+    for t in (0.0, -0.0, 0, 2.0 ** -64, 2.0 ** 100, 1):
+        P.verify_drafts(z, *args, temperature=t)
+    P.op_status()
