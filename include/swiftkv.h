@@ -649,7 +649,7 @@ int32_t swiftkv_token_logprobs_bwd(const void *logits, int64_t row_stride, int32
  *   tokens_out  : int32 [n_seqs][max_new]: the standing tokens, the next token, -1 behind it
  *   path        : int32 [n_seqs][max_new]: places in the sequence of the first new token (0) and of the standing ones, -1 behind them
  * A sequence without new tokens: n_accepted 0, -1 everywhere.  A row with NaN or +inf, or without any finite logit, is decided as with T = 0 (NaN
- * counts as the largest).  A token whose w is below 2^-1000 has none; denormal logits count as 0.  cu_new outside [0, total_new], and new tokens beyond max_new, are not
+ * counts as the largest).  A token whose w is below 2^-1000 has none; denormal logits, probabilities and random numbers count as 0.  cu_new outside [0, total_new], and new tokens beyond max_new, are not
  * followed, and reported.  Sums, products and comparisons are those of 64-bit arithmetic on the given values: where
  * 32 bits decide beyond doubt they are not formed.  Deterministic.  No output may overlap an input or another output.
  * 1 <= max_new <= 1024, vocab <= 2^30, n_seqs <= 2^24.  Errors: INVALID_ARG, CUDA. */

@@ -19,8 +19,8 @@
 //   the difference z - r, its product with c and c itself are rounded (3 x 2^-24 |t| ln 2 relative, t the exponent; over a row the mean of |t| weighted
 //   with w is at most log2(vocab) <= 30: 4e-6), the approximate exponential has 2^-22, a thread's sums have (32 + chunks) 2^-24, and its reference moves
 //   at most once a chunk, and three times when parts are joined, by a factor that is off by 2^-22: 2^-16 + (chunks + 4) 2^-21 covers them.
-//   A token's own w is off by 1.3e-7 |t|, at most 1.6e-5 where it is not zero.
-// A decision whose two sides are nearer to each other than twice that is taken again with the row's sum in 64 bits (a few in 10^4).
+//   A token's own w is off by 1.3e-7 |t|, at most 1.6e-5 where it is not zero; where it is, it is below 2^-126.
+// A decision whose two sides are nearer to each other than twice that (and than 2^-126) is taken again with the row's sum in 64 bits (a few in 10^4).
 // A token is drawn from sums in 64 bits: the borders between tokens lie 1 / vocab apart, nearer than 32 bits resolve.  The power of
 // two is there 2^(n / 16), of a table of 16, times a polynomial of the 5th degree (1e-14): 13 operations of the 64-bit units for
 // a token instead of 18 without the table.
@@ -427,7 +427,7 @@ __device__ __forceinline__ int vd_children(const VdDrafts &d, const double *root
     if (certain && several) sofar = warp_prefix64((double)w) - (double)w;
     const double left = certain ? (double)total - (gone + sofar) : (double)total * q;
     const double diff = (double)w - (double)u * left;
-    const double near = EXACT ? 0.0 : 2.0 * a.unsure * ((double)w + (double)u * (certain ? (double)total : left));
+    const double near = EXACT ? 0.0 : 2.0 * a.unsure * ((double)w + (double)u * (certain ? (double)total : left)) + 0x1p-126;
     const unsigned stands = __ballot_sync(0xffffffffu, is && diff > near);
     const unsigned open = __ballot_sync(0xffffffffu, is && !EXACT && !(diff > near) && !(diff < -near) && !again);
     if (stands | open) {

@@ -210,3 +210,16 @@ def test_verify_drafts_refuses_temperatures_that_32_bits_round_to_0():
     for t in (0.0, -0.0, 0, 2.0 ** -64, 2.0 ** 100, 1):
         P.verify_drafts(z, *args, temperature=t)
     P.op_status()
+
+
+@pytest.mark.parametrize("n_seqs,vocab", [(6, 300), (6, 40000), (200, 3000)])
+def test_verify_drafts_weights_below_the_range_of_32_bits(n_seqs, vocab):
+    """Drafted tokens whose weight is below 2^-126 against products of a small random number and a small probability: 64 bits decide."""
+    z = torch.full((2 * n_seqs, vocab), -500.0, device="cuda")
+    z[:, 3] = 0.0
+    at = torch.arange(n_seqs, device="cuda") % 3
+    z[0::2, 7] = f32([-95.0, -103.0, -90.0])[at]
+    q = torch.full((2 * n_seqs, vocab), 2.0 ** -120, device="cuda")
+    u = torch.full((2 * n_seqs,), 2.0 ** -24, device="cuda")
+    counts, _, _ = T.check_verify(z, np.full(2 * n_seqs, 7), 2 * np.arange(n_seqs + 1), None, q, u)
+    assert counts.tolist() == [[1, 0, 1][b % 3] for b in range(n_seqs)]
