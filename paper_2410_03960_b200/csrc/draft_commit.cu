@@ -23,7 +23,7 @@ constexpr int CD_PLANES = 224;               // of one launch: what its paramete
 struct CommitArgs {
   const int32_t *table, *row0, *past, *accepted, *path;
   int32_t *past_out;
-  int max_blocks, max_new, cache_rows, n_seqs, last;
+  int max_blocks, max_new, cache_rows, last;
   unsigned int *status;
 };
 struct CommitPlanes {
@@ -159,7 +159,7 @@ extern "C" int32_t swiftkv_commit_drafts(void *const *planes, const int64_t *row
   unsigned int *status = op_status_word();
   if (!status) return report_error(SWIFTKV_ERR_CUDA, "no status word");
   cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
-  CommitArgs a{block_table, row0, n_past, n_accepted, path, n_past_out, max_blocks, max_new, cache_rows, n_seqs, 0, status};
+  CommitArgs a{block_table, row0, n_past, n_accepted, path, n_past_out, max_blocks, max_new, cache_rows, 0, status};
   int done = 0;
   do {
     CommitPlanes part;

@@ -92,8 +92,8 @@ struct alignas(16) TdRow {                               // what the two kinds o
 };
 struct TdShared {
   TdRow row[TD_ROWS];
-  TdPart part[2][TD_MAX_CLUSTER];
-  uint64_t full[TD_STAGES], ready[TD_STAGES], empty[TD_STAGES], given[TD_ROWS], weighed[TD_ROWS], summed[TD_ROWS], joined[TD_ROWS], left[TD_ROWS], met[2];
+  TdPart part[TD_MAX_CLUSTER];               // of the row that a cluster's blocks share (it has one)
+  uint64_t full[TD_STAGES], ready[TD_STAGES], empty[TD_STAGES], given[TD_ROWS], weighed[TD_ROWS], summed[TD_ROWS], joined[TD_ROWS], left[TD_ROWS], met;
   int known;                                 // the last row (of the block's, counted) whose tokens are known
 };
 
@@ -364,7 +364,7 @@ __global__ void __launch_bounds__(TD_THREADS + 96, 2) topk_distill_kernel(const 
       tc::mbar_init(tc::smem_u32(&sh.empty[i]), TD_WARPS);
     }
     sh.known = -1;
-    for (int i = 0; i < 2; ++i) tc::mbar_init(tc::smem_u32(&sh.met[i]), a.splits);
+    tc::mbar_init(tc::smem_u32(&sh.met), a.splits);
     for (int i = 0; i < TD_ROWS; ++i) {
       tc::mbar_init(tc::smem_u32(&sh.given[i]), 1);
       tc::mbar_init(tc::smem_u32(&sh.weighed[i]), 1);
@@ -500,19 +500,19 @@ __global__ void __launch_bounds__(TD_THREADS + 96, 2) topk_distill_kernel(const 
       const TdEntries now = r.e;
       TdPart all = td_warp_join(lane < TD_WARPS ? r.warp[lane] : TdPart{-INFINITY, 0.f}, c);
       if (a.splits > 1) {
-        // to every block of the cluster; each waits for all.  (What it got two rows ago it has read before it sent its part of the row in between.)
+        // to every block of the cluster; each waits for all
         if (lane < a.splits) {
           TdShared *const peer = cg::this_cluster().map_shared_rank(&sh, lane);
-          peer->part[turn & 1][part] = all;
-          cluster_arrive(tc::smem_u32(&sh.met[turn & 1]), lane);
+          peer->part[part] = all;
+          cluster_arrive(tc::smem_u32(&sh.met), lane);
         }
         __syncwarp();
-        if (alive && !cluster_wait(tc::smem_u32(&sh.met[turn & 1]), (turn >> 1) & 1)) {
+        if (alive && !cluster_wait(tc::smem_u32(&sh.met), 0)) {
           alive = false;
           atomicOr(a.status, STATUS_TIMEOUT);
         }
         alive = __all_sync(0xffffffffu, alive);
-        all = td_warp_join(lane < a.splits ? sh.part[turn & 1][lane] : TdPart{-INFINITY, 0.f}, c);
+        all = td_warp_join(lane < a.splits ? sh.part[lane] : TdPart{-INFINITY, 0.f}, c);
       }
       const TdOutcome o = td_outcome(now, all, a);
       // (one logarithm for all)
