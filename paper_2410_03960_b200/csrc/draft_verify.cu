@@ -899,8 +899,11 @@ template <typename T>
 cudaError_t launch_verify(VdArgs a, int n_seqs, cudaStream_t st) {
   static_assert(sizeof(VdShared) <= 32 * 1024, "shared memory");
   // a sequence gets a cluster of as many blocks as run at once with all the others' (16 at most), each with thousands of logits of a row, and of at least so
-  // many that none has more than 256 KB of it (256 sequences of 100003 fp32: 128 us with two blocks each in two turns, 137 us with one each; 128
-  // sequences of 128256 bf16 with two 96 us, with four 100 us)
+  // many that none has more than 256 KB of it.  Both sides of that border, chains of 4 tokens, us with one block a sequence / with two: below it 200 x 131000 bf16 112 / 102,
+  // 256 sequences 113 / 114, 400 sequences 184 / 159; above it 200 x 133000 117 / 110, 256 117 / 121, 400 187 / 171; fp32 200 x 67000 81 / 82, 256 83 / 97, 400 138 / 133,
+  // 200 x 100003 118 / 108, 256 113 / 126, 400 179 / 171, but 256 of 1 - 6 tokens 137 / 126.  It gains up to a tenth where two turns of blocks are needed anyway, and loses
+  // up to a sixth of fp32 rows just above it where one block each fits in one turn; a border at half of that loses a sixth at 128 sequences (133000 bf16: 69 with
+  // two blocks, 82 with four).
   static_assert(1 << 4 == VD_MAX_CLUSTER, "from the largest cluster down");
   for (a.log_splits = 4; a.log_splits > 0; --a.log_splits)
     if (a.vocab >> a.log_splits >= 2048 && (n_seqs <= verify_clusters<T>(a.log_splits) || ((long long)a.vocab * (long long)sizeof(T)) >> (a.log_splits - 1) > 262144)) break;
