@@ -639,8 +639,8 @@ int32_t swiftkv_token_logprobs_bwd(const void *logits, int64_t row_stride, int32
  *                 (at or beyond vocab: reported)
  *   parents     : int32 [total_new], parent's place in the sequence, below the token's own (others: the token is never reached, and reported;
  *                 a sequence's first entry is not looked at).  Null: every token's parent is the one before it
- *   draft_probs : fp32 [total_new][vocab], draft_stride elements between rows (a sequence's first row and those of ids outside [0, vocab) are not looked at; values below 0
- *                 and NaN count as 0), or null: the drafter chose for certain.  Chains only: not together with parents
+ *   draft_probs : fp32 [total_new][vocab], draft_stride elements between rows (a sequence's first row and those of ids outside [0, vocab) are not
+ *                 looked at; values below 0 and NaN count as 0), or null: the drafter chose for certain.  Chains only: not together with parents
  *   uniforms    : fp32 [total_new]; below 0 and NaN count as 0, 1 and above as the largest number below 1.  May be null where `temperatures` is
  *                 and temperature is 0
  *   temperatures: fp32 [n_seqs], or null: `temperature` for all.  0, or in [2^-64, 2^100]; anything else on the device counts as 0 and is
@@ -650,7 +650,7 @@ int32_t swiftkv_token_logprobs_bwd(const void *logits, int64_t row_stride, int32
  *   path        : int32 [n_seqs][max_new]: places in the sequence of the first new token (0) and of the standing ones, -1 behind them
  * A sequence without new tokens: n_accepted 0, -1 everywhere.  A row with NaN or +inf, or without any finite logit, is decided as with T = 0 (NaN
  * counts as the largest).  A token whose w is below 2^-1000 has none; denormal logits, probabilities and random numbers count as 0.  cu_new outside [0, total_new], and new tokens beyond max_new, are not
- * followed, and reported.  Sums, products and comparisons are those of 64-bit arithmetic on the given values: where
+ * followed, and reported.  Sums, products and comparisons are those of 64-bit arithmetic on the given values (exponentials to 1e-14 of themselves): where
  * 32 bits decide beyond doubt they are not formed.  Deterministic.  No output may overlap an input or another output.
  * 1 <= max_new <= 1024, vocab <= 2^30, n_seqs <= 2^24.  Errors: INVALID_ARG, CUDA. */
 int32_t swiftkv_verify_drafts(const void *logits, int64_t row_stride, int32_t dtype, const int32_t *tokens, const int32_t *cu_new,

@@ -11,7 +11,7 @@
 // What bounds it: a sequence's chain of steps, not HBM.  Per group of rows an exchange and its verdicts (3 us), at the end one pass over the last row's
 // weights in 64 bits, two with the drafter's probabilities (3 elements per clock and SM of the 4.9 that the 64-bit units give; 10 us each for 128256 logits in four
 // blocks), and the search of the token (2.5 us).  Measured at 128256 bf16 logits (device time, graph): 1 sequence x 5 tokens 18 us, 8 x 8 27 us, 16 trees of
-// up to 32 tokens 27 us, 64 x 8 with the drafter's probabilities 68 us (104 MB read); 256 x 6 fp32 of 100003 126 us (246 MB).  Tried and slower: a second
+// up to 32 tokens 27 us, 64 x 8 with the drafter's probabilities 69 us (104 MB read), without 52 us, greedy 34 us; 256 x 6 fp32 of 100003 125 us (246 MB).  Tried and slower: a second
 // kernel for the draw (64 x 8 76 - 94 us), a ninth warp that fills the ring (76 us, registers spill), blocks of 512 threads (68 - 88 us), two steps of a
 // tile at once (74 us), the search over the pass's own code (75 us), three blocks per SM (89 us).
 //

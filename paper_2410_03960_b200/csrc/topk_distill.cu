@@ -13,12 +13,12 @@
 // Blocks are persistent and stream rows through a ring of 32 KB bulk copies.  One warp feeds the ring and blanks, so that the reading warps need no barrier
 // among themselves (4096 rows bf16: 210 us with one per chunk, 178 without); another reads the entries of up to four rows ahead, and a third joins up finished
 // rows (where rows are short these two are what a block waits for: 4096 x 1252 bf16 of 100 entries 75 us, 80 with one warp for both; with the gradient 76 and 93).  With the gradient a row is looked at twice: its last three chunks are still in the ring, and the lines of the others are kept in L2
-// (evict_last; all else evict_first), so that HBM sees hardly more than one read and one write (579 + 467 MB for 2 x 525; without the hints
+// (evict_last; all else evict_first), so that HBM sees hardly more than one read and one write (581 + 466 MB for 2 x 525; without the hints
 // 881 MB are read).  Few rows: a cluster of up to 8 blocks shares a row.
 //
-// What bounds it: HBM for the loss alone, the exponential units (72 %) close behind for 16-bit logits: 4096 x 128256 bf16 178 us (5.9 TB/s), 1024 x 128256 fp32
+// What bounds it: HBM for the loss alone, the exponential units (71 %) close behind for 16-bit logits: 4096 x 128256 bf16 178 - 181 us (5.9 TB/s), 1024 x 128256 fp32
 // 81 us (6.5 TB/s).  With the gradient the join between a row's two looks, behind which two blocks per SM hide one another only in part: 2048 x 128256
-// bf16 211 us (5.0 TB/s); the gradient alone 169 us (6.2 TB/s).  33 rows fp32 7.7 us.  Tried and slower: rows split over two blocks
+// bf16 211 - 216 us (5.0 TB/s); the gradient alone 170 us (6.2 TB/s), 1024 x 128256 fp32 174 us.  33 rows fp32 7.7 us.  Tried and slower: rows split over two blocks
 // (248 us), one block per SM with twice the ring (239 us), chunks of half the size (233 against 221 us).
 #include <cooperative_groups.h>
 
@@ -689,7 +689,7 @@ __global__ void __launch_bounds__(TD_THREADS + 96, 2) topk_distill_kernel(const 
   }
 }
 
-// The gradient alone: elementwise, one read and one write, vectors on the output's 16-byte boundaries.  EVEN: these are the input's too.  2048 x 128256 bf16 169 us
+// The gradient alone: elementwise, one read and one write, vectors on the output's 16-byte boundaries.  EVEN: these are the input's too.  2048 x 128256 bf16 170 us
 // (6.2 TB/s; 212 us with the loads behind the entries and half the work per block); 1000 x 100001 with other strides 80 us, 69 us where rows are even
 constexpr int TB_THREADS = 256, TB_UNROLL = 8;
 struct TdBwdArgs {
