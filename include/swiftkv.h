@@ -689,7 +689,7 @@ int32_t swiftkv_commit_drafts(void *const *planes, const int64_t *row_bytes, int
  * (1, but where sum p_k > 1 by more than 2^-17, what rounded log probabilities may be off by; where the others are masked; and where no p_k is above 0 at
  * rest == 0), with q_k = exp(z_k - lse), q_r = exp(rest_lse - lse) of z_k as the fp32 product of logit and 1 / T and of the log sums as they are returned
  * (where they are below 64), from one pass over HBM: the second look at a row is served by the L2 cache.  Sums over the other tokens are fp32, with the
- * GPU's approximate exponentials (2^-22); what is formed of them and the entries is 64-bit.  Repeats bit for bit.
+ * GPU's approximate exponentials (2^-22, 0 below 2^-126); what is formed of them and the entries is 64-bit.  Repeats bit for bit.
  * rows <= 2^26, vocab <= 2^30.  Errors: INVALID_ARG, CUDA. */
 int32_t swiftkv_topk_distill(const void *logits, int64_t row_stride, int32_t dtype, const int32_t *top_ids, const float *top_logprobs,
                              int32_t rows, int32_t vocab, int32_t top_k, double temperature, int32_t rest, float *loss, float *lse,
