@@ -696,7 +696,7 @@ int32_t swiftkv_topk_distill(const void *logits, int64_t row_stride, int32_t dty
                              float *rest_lse, const float *grad_loss, void *grad_logits, int64_t grad_stride, void *cuda_stream);
 
 /* The gradient alone, from the lse and rest_lse that the forward call gave.  Where these are so large that fp32 does not resolve them (z / T beyond 10^5), exponents
- * are off by as much, those of the others to the lower side: no q_k and no term of the others' softmax comes out above 1. */
+ * are off by as much, those of the others to the lower side: no q_k and no term of the others' softmax comes out above 1 by more than 2^-5. */
 int32_t swiftkv_topk_distill_bwd(const void *logits, int64_t row_stride, int32_t dtype, const int32_t *top_ids, const float *top_logprobs,
                                  int32_t rows, int32_t vocab, int32_t top_k, double temperature, int32_t rest, const float *lse,
                                  const float *rest_lse, const float *grad_loss, void *grad_logits, int64_t grad_stride,

@@ -286,7 +286,7 @@ struct TdOutcome {
   float top;               // the row's largest logit
   double total, rest;      // sum of weights relative to it, and the others'
   double p_r, norm;        // the others' probability, and what the entries' are divided by
-  double mass;             // what all outcomes' then sum to
+  double mass;             // what all outcomes have together
   double f;                // the entries' weights are relative to their own largest: times this
   bool some;               // there are others that are not masked
 };
@@ -764,7 +764,7 @@ __global__ void __launch_bounds__(TB_THREADS) topk_distill_bwd_kernel(TdBwdArgs 
   if (tid == 0) s_mass = mass;
   const float scale = some ? (float)((double)g * (mass * exp((double)rest_lse - (double)lse) - p_r) * a.inv_t) : 0.f;
   const float c = (float)(1.4426950408889634 * a.inv_t);
-  // No term of a softmax is above 1: a reference that does not resolve that (2^18: exponents off by 3 x 2^-6) is raised by what rest_lse, it and c may be rounded by
+  // No term of a softmax is above 1: a reference that does not resolve that (from 2^18 on: exponents off by 3 x 2^-6) is raised by what rest_lse, it and c may be rounded by
   const float near_ref = (float)(1.4426950408889634 * (double)rest_lse), ref = fabsf(near_ref) > 0x1p18f ? near_ref + fabsf(near_ref) * 0x1p-22f : near_ref;
   const bool sloped = any && some;                         // (no entries, or others that are masked, be they finite and large: 0)
   auto slope = [&](float v) { return sloped ? scale * exp2_approx(fmaf(v, c, -ref)) : 0.f; };
@@ -792,7 +792,7 @@ __global__ void __launch_bounds__(TB_THREADS) topk_distill_bwd_kernel(TdBwdArgs 
   __syncthreads();
   if (id >= e0 && id < e1) {
     const double t = (double)z * a.inv_t + td_rounding(z, a.inv_t) - (double)lse;
-    const bool above = __double2hiint(t) >= 0x3f900000 && __double2hiint(t) <= 0x7ff00000;      // (2^-6 to infinity: likewise)
+    const bool above = __double2hiint(t) >= 0x3f900000 && __double2hiint(t) <= 0x7ff00000;      // (2^-6 to infinity: an entry's likewise; what is less is the rounding of an ordinary lse)
     lp_store(y + id, (float)((double)g * (s_mass * exp(above ? 0.0 : t) - p / norm) * a.inv_t));
   }
 }
